@@ -464,6 +464,105 @@ gpulet_status gpulet_fc(const void *x, const void *w, const float *b, void *y, i
 gpulet_status gpulet_fc_static_scratch(const void *x, const void *w, const float *b, void *y, int N, int In,
                                        int Out, int relu, int out_fp32, void *stream);
 
+/* Element types of the layers below. */
+enum { GPULET_BF16 = 0, GPULET_F16 = 1, GPULET_F32 = 2 };
+
+/* Activations of the layers below, on the fp32 value before it is rounded:
+ *   RELU max(v, 0) (NaN stays NaN)      SILU v / (1 + exp(-v))
+ *   GELU v * Phi(v), Phi the normal distribution function
+ *   GELU_TANH v / 2 * (1 + tanh(sqrt(2 / pi) * (v + 0.044715 v^3))) */
+enum { GPULET_ACT_NONE = 0, GPULET_ACT_RELU = 1, GPULET_ACT_SILU = 2, GPULET_ACT_GELU = 3, GPULET_ACT_GELU_TANH = 4 };
+
+/*
+ * Matrix product on MFMA with bias, residual and activation in its epilogue:
+ *   y[m,n] = act(sum_k x[m,k] * w[n,k] + b[n] + residual[m,n])
+ * for layers that work row by row (the pixels of a map, a batch of feature
+ * vectors): one row or millions, any width, rows dense or slices of wider ones.
+ * x: M rows of K, w: N rows of K ([Out][In], as gpulet_fc), both of `dtype`
+ * (GPULET_BF16 or GPULET_F16); b: N fp32 or NULL; residual: NULL or M rows of N
+ * of out_dtype; y: M rows of N of out_dtype, which is dtype or GPULET_F32.
+ * ldx, ldw, ldr, ldy: elements from one row to the next, 0 = dense; a slice of
+ * wider rows is given by the address of its first element and the wide rows' ld.
+ * Elements of y's rows behind column N are left as they were.
+ * Sums, bias, residual and activation are fp32, y is rounded once.  Same call on
+ * the same number of CUs, same bits; the order of the sum (not more) may differ
+ * between values of M, N, K, alignments and gpu-let sizes.  Products of infinities
+ * and NaN in x or w follow IEEE arithmetic in the rows and columns they belong
+ * to, and reach no others.
+ * y may be the residual itself (same address, ld); otherwise y may share no
+ * element with x, w, b or residual (column slices of the same wide rows are
+ * told apart).  Fastest where rows start at multiples of 16 bytes.
+ * Errors: GPULET_EINVAL for a NULL descriptor, x, w or y; M, N or K below 1; M
+ * above 2^24, N, K or an ld above 2^20, 64 x 64 tiles of y beyond 2^23; an ld
+ * below the row's width; an unknown type or activation; a pointer that is not a
+ * multiple of its element's size; overlap as above.  GPULET_EINVAL also for a
+ * workspace that is not 256-byte aligned or overlaps an operand.
+ */
+typedef struct gpulet_matmul_desc {
+    const void *x, *w;
+    const float *b;
+    const void *residual;
+    void *y;
+    int32_t M, N, K;
+    int32_t ldx, ldw, ldr, ldy;
+    int32_t dtype, out_dtype, act;
+} gpulet_matmul_desc;
+
+/* Bytes of workspace with which gpulet_matmul is fastest on any number of CUs (0
+ * for most shapes: it is for few rows and a long K, whose depth is split over
+ * workgroups).  Needs no GPU.  Errors as gpulet_matmul. */
+gpulet_status gpulet_matmul_workspace_bytes(const gpulet_matmul_desc *d, size_t *bytes);
+
+/* Enqueues the product on `stream`.  `workspace` is device memory of
+ * workspace_bytes bytes that nothing else uses until the work is done (calls on
+ * one stream may share it, graphs that may run at the same time may not); what it
+ * holds before does not matter.  NULL or fewer bytes than asked for are allowed:
+ * the depth is then split less or not at all. */
+gpulet_status gpulet_matmul(const gpulet_matmul_desc *d, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Group norm over NHWC maps with residual and activation:
+ *   y = act((x - mean) / sqrt(var + eps) * gamma[c] + beta[c] + residual)
+ * mean and var = mean((x - mean)^2) over the H * W * C / groups values of an
+ * image's group of C / groups consecutive channels (groups = 1: all of them,
+ * groups = C: each channel by itself).
+ * x, residual (or NULL), y: N*H*W pixels of C channels of `dtype` (GPULET_BF16,
+ * GPULET_F16, GPULET_F32); gamma, beta: C fp32, NULL = 1 and 0.
+ * x_ch_stride, r_ch_stride, y_ch_stride: channels per stored pixel, 0 = C; a
+ * channel slice of wider pixels is given by the address of its first element.
+ * Other channels of y's pixels are left as they were.
+ * Statistics and everything up to the one rounding of y are fp32, the variance
+ * from differences to the mean.  An image's result does not depend on the batch
+ * it is part of or on the gpu-let.  An infinity or NaN makes its group's
+ * outputs in its image NaN and reaches no other group or image.  A group whose
+ * values are all equal gives act(beta + residual); with eps = 0 its outputs are NaN.
+ * y may be x itself or the residual itself (same address, ch_stride); otherwise y
+ * may share no element with x, residual, gamma or beta.
+ * Errors: GPULET_EINVAL for a NULL descriptor, x or y; non-positive sizes; groups
+ * that do not divide C; a ch_stride below C; an image of 2^31 bytes or more
+ * (counting the stored pixels); more than 2^22 (image, group) pairs; a negative,
+ * infinite or NaN eps; an unknown type or activation; misaligned pointers and
+ * overlap as gpulet_matmul.  GPULET_ENOMEM when workspace_bytes is less than
+ * gpulet_group_norm_workspace_bytes says.
+ */
+typedef struct gpulet_group_norm_desc {
+    const void *x;
+    const float *gamma, *beta;
+    const void *residual;
+    void *y;
+    int32_t N, C, H, W, groups;
+    int32_t x_ch_stride, r_ch_stride, y_ch_stride;
+    float eps;
+    int32_t dtype, act;
+} gpulet_group_norm_desc;
+
+/* Bytes of workspace gpulet_group_norm needs (0 for maps whose groups fit into
+ * registers).  Needs no GPU.  Errors as gpulet_group_norm. */
+gpulet_status gpulet_group_norm_workspace_bytes(const gpulet_group_norm_desc *d, size_t *bytes);
+
+/* Enqueues the layer on `stream`; `workspace` as in gpulet_matmul, but needed. */
+gpulet_status gpulet_group_norm(const gpulet_group_norm_desc *d, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------------------------
  * Whole model on a gpu-let (Sec. 5 "Backend inference executor").
  * ------------------------------------------------------------------------ */

@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libgpulet.so")
 
 SOURCES = ["mask.cpp", "partition.cpp", "layers.cpp", "model.cpp", "sched.cpp", "interference.cpp", "conv.hip",
            "conv_igemm.hip", "conv_patch.hip", "conv_tall.hip", "conv_stream.hip", "conv_stem.hip", "conv_pooled.hip", "conv_dwpw.hip", "dwconv.hip", "image_chain.hip",
-           "pool.hip", "fc.hip", "probe.hip"]
+           "pool.hip", "fc.hip", "matmul.hip", "group_norm.hip", "probe.hip"]
 
 # The scheduler's fp64 decisions must not depend on fused multiply-adds.
 EXTRA = {"sched.cpp": ["-ffp-contract=off"], "interference.cpp": ["-ffp-contract=off"]}

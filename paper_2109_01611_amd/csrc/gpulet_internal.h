@@ -137,6 +137,33 @@ hipError_t launch_fc_static(const void *x, const void *w, const float *b, void *
 hipError_t launch_dwconv(const void *x, const void *w, const float *b, void *y, int N, int C, int H, int W,
                          int R, int S, int stride, int pad, int relu, int P, int Q, hipStream_t stream);
 
+// matmul.hip and group_norm.hip.  Arguments are those of the descriptors with every stride filled in.
+struct MatmulArgs {
+    const void *x, *w;
+    const float *b;
+    const void *residual;
+    void *y;
+    int M, N, K, ldx, ldw, ldr, ldy, dtype, out_dtype, act;
+    void *ws;
+    size_t ws_bytes;
+};
+gpulet_status check_matmul(const gpulet_matmul_desc *d, MatmulArgs &a);
+size_t matmul_workspace(const MatmulArgs &a);   // most bytes launch_matmul can use, whatever the CU count
+hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream);
+struct GroupNormArgs {
+    const void *x;
+    const float *gamma, *beta;
+    const void *residual;
+    void *y;
+    int N, C, H, W, groups, ldx, ldr, ldy, dtype, act;
+    float eps;
+    void *ws;
+    size_t ws_bytes;
+};
+gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a);
+size_t group_norm_workspace(const GroupNormArgs &a);   // bytes launch_group_norm needs
+hipError_t launch_group_norm(const GroupNormArgs &a, const LaunchCtx &ctx, hipStream_t stream);
+
 // image_chain.hip: consecutive small layers, each reading what the one before wrote, as one launch with one
 // workgroup per image.  Every layer takes (C, H, W) to (K, P, Q) per image: convolutions with dense input and
 // output, max pools (R x R windows, K = C), fully connected layers (K outputs, P = Q = 1).  `y` is where the

@@ -2,6 +2,7 @@
 // the caller's stream (paper Sec. 5: the executor runs the model's layers on
 // its gpu-let).
 #include <cstdint>
+#include <initializer_list>
 
 #include "gpulet_internal.h"
 
@@ -23,7 +24,151 @@ gpulet_status make_conv_args(ConvArgs &a, const void *x, const void *w, const fl
     return check_conv(a);
 }
 
+// `rows` rows of `width` bytes, `pitch` bytes apart.
+struct Rows {
+    uintptr_t at;
+    uint64_t rows, width, pitch;
+    uint64_t span() const { return rows ? (rows - 1) * pitch + width : 0; }
+};
+Rows make_rows(const void *p, uint64_t rows, uint64_t width, uint64_t pitch) {
+    return Rows{reinterpret_cast<uintptr_t>(p), p ? rows : 0, width, pitch};
+}
+
+// Whether the two share a byte.  Slices of the same wide rows (equal pitches) are compared by their columns; rows of
+// different pitches count as sharing where their address ranges meet.
+bool meet(const Rows &a, const Rows &b) {
+    if (a.span() == 0 || b.span() == 0) return false;
+    if (a.at >= b.at + b.span() || b.at >= a.at + a.span()) return false;
+    if (a.pitch != b.pitch) return true;
+    const uint64_t d = a.at <= b.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
+    // in a's frame a covers columns [0, a.width), b covers [d, d + b.width), wrapping into the next row
+    return d < a.width || d + b.width > a.pitch;
+}
+
+gpulet_status check_workspace(const void *ws, size_t bytes) {
+    return bytes > 0 && ws && reinterpret_cast<uintptr_t>(ws) % 256 != 0 ? GPULET_EINVAL : GPULET_OK;
+}
+
+constexpr int kMaxRow = 1 << 20;   // elements: 256 rows of fp32 stay below 2^31 bytes
+
+int type_bytes(int t) { return t == GPULET_F32 ? 4 : 2; }
+bool misaligned(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % static_cast<unsigned>(bytes) != 0; }
+
 }  // namespace
+
+namespace gpulet {
+
+gpulet_status check_matmul(const gpulet_matmul_desc *d, MatmulArgs &a) {
+    if (!d || !d->x || !d->w || !d->y) return GPULET_EINVAL;
+    if (d->M < 1 || d->N < 1 || d->K < 1 || d->M > (1 << 24) || d->N > kMaxRow || d->K > kMaxRow) return GPULET_EINVAL;
+    if ((d->M + 63LL) / 64 * ((d->N + 63LL) / 64) > (1 << 23)) return GPULET_EINVAL;
+    if (d->dtype != GPULET_BF16 && d->dtype != GPULET_F16) return GPULET_EINVAL;
+    if (d->out_dtype != d->dtype && d->out_dtype != GPULET_F32) return GPULET_EINVAL;
+    if (d->act < GPULET_ACT_NONE || d->act > GPULET_ACT_GELU_TANH) return GPULET_EINVAL;
+    a = MatmulArgs{d->x, d->w, d->b, d->residual, d->y, d->M, d->N, d->K, d->ldx ? d->ldx : d->K, d->ldw ? d->ldw : d->K,
+                   d->ldr ? d->ldr : d->N, d->ldy ? d->ldy : d->N, d->dtype, d->out_dtype, d->act, nullptr, 0};
+    if (a.ldx < a.K || a.ldw < a.K || a.ldr < a.N || a.ldy < a.N) return GPULET_EINVAL;
+    if (a.ldx > kMaxRow || a.ldw > kMaxRow || a.ldr > kMaxRow || a.ldy > kMaxRow) return GPULET_EINVAL;
+    const int es = type_bytes(a.out_dtype);
+    if (misaligned(a.x, 2) || misaligned(a.w, 2) || misaligned(a.b, 4) || misaligned(a.residual, es) || misaligned(a.y, es))
+        return GPULET_EINVAL;
+    const uint64_t M = a.M, N = a.N, K = a.K;
+    const Rows y = make_rows(a.y, M, es * N, 1ull * es * a.ldy), r = make_rows(a.residual, M, es * N, 1ull * es * a.ldr);
+    if (meet(y, make_rows(a.x, M, 2 * K, 2ull * a.ldx)) || meet(y, make_rows(a.w, N, 2 * K, 2ull * a.ldw)) ||
+        meet(y, make_rows(a.b, 1, 4 * N, 4 * N)))
+        return GPULET_EINVAL;
+    if (!(a.residual == a.y && a.ldr == a.ldy) && meet(y, r)) return GPULET_EINVAL;
+    return GPULET_OK;
+}
+
+gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a) {
+    if (!d || !d->x || !d->y) return GPULET_EINVAL;
+    if (d->N < 1 || d->C < 1 || d->H < 1 || d->W < 1 || d->groups < 1 || d->C % d->groups != 0) return GPULET_EINVAL;
+    if (d->dtype < GPULET_BF16 || d->dtype > GPULET_F32 || d->act < GPULET_ACT_NONE || d->act > GPULET_ACT_GELU_TANH)
+        return GPULET_EINVAL;
+    if (!(d->eps >= 0.f) || d->eps > 3.0e38f) return GPULET_EINVAL;
+    if (1LL * d->N * d->groups > (1 << 22)) return GPULET_EINVAL;
+    a = GroupNormArgs{d->x, d->gamma, d->beta, d->residual, d->y, d->N, d->C, d->H, d->W, d->groups,
+                      d->x_ch_stride ? d->x_ch_stride : d->C, d->r_ch_stride ? d->r_ch_stride : d->C,
+                      d->y_ch_stride ? d->y_ch_stride : d->C, d->dtype, d->act, d->eps, nullptr, 0};
+    if (a.ldx < a.C || a.ldr < a.C || a.ldy < a.C) return GPULET_EINVAL;
+    const int es = type_bytes(a.dtype);
+    const long long px = 1LL * a.H * a.W;
+    for (int ld : {a.ldx, a.ldr, a.ldy})
+        if (px >= (1LL << 31) || px * ld >= (1LL << 31) / es) return GPULET_EINVAL;
+    if (misaligned(a.x, es) || misaligned(a.residual, es) || misaligned(a.y, es) || misaligned(a.gamma, 4) || misaligned(a.beta, 4))
+        return GPULET_EINVAL;
+    const uint64_t all = 1ull * a.N * px, C = a.C;
+    const Rows y = make_rows(a.y, all, es * C, 1ull * es * a.ldy);
+    if (meet(y, make_rows(a.gamma, 1, 4 * C, 4 * C)) || meet(y, make_rows(a.beta, 1, 4 * C, 4 * C))) return GPULET_EINVAL;
+    if (!(a.x == a.y && a.ldx == a.ldy) && meet(y, make_rows(a.x, all, es * C, 1ull * es * a.ldx))) return GPULET_EINVAL;
+    if (!(a.residual == a.y && a.ldr == a.ldy) && meet(y, make_rows(a.residual, all, es * C, 1ull * es * a.ldr)))
+        return GPULET_EINVAL;
+    return GPULET_OK;
+}
+
+}  // namespace gpulet
+
+extern "C" gpulet_status gpulet_matmul_workspace_bytes(const gpulet_matmul_desc *d, size_t *bytes) {
+    if (!bytes) return GPULET_EINVAL;
+    MatmulArgs a;
+    const gpulet_status st = check_matmul(d, a);
+    if (st == GPULET_OK) *bytes = matmul_workspace(a);
+    return st;
+}
+
+extern "C" gpulet_status gpulet_matmul(const gpulet_matmul_desc *d, void *workspace, size_t workspace_bytes, void *stream) {
+    MatmulArgs a;
+    gpulet_status st = check_matmul(d, a);
+    if (st == GPULET_OK && workspace) {
+        a.ws = workspace;
+        a.ws_bytes = workspace_bytes;
+        st = check_workspace(workspace, workspace_bytes);
+        const int es = type_bytes(a.out_dtype);
+        const Rows ws = make_rows(workspace, 1, workspace_bytes, workspace_bytes);
+        if (meet(ws, make_rows(a.x, a.M, 2ull * a.K, 2ull * a.ldx)) || meet(ws, make_rows(a.w, a.N, 2ull * a.K, 2ull * a.ldw)) ||
+            meet(ws, make_rows(a.b, 1, 4ull * a.N, 4ull * a.N)) ||
+            meet(ws, make_rows(a.residual, a.M, 1ull * es * a.N, 1ull * es * a.ldr)) ||
+            meet(ws, make_rows(a.y, a.M, 1ull * es * a.N, 1ull * es * a.ldy)))
+            return GPULET_EINVAL;
+    }
+    if (st != GPULET_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    GPULET_HIP(launch_matmul(a, stream_ctx(s), s));
+    return GPULET_OK;
+}
+
+extern "C" gpulet_status gpulet_group_norm_workspace_bytes(const gpulet_group_norm_desc *d, size_t *bytes) {
+    if (!bytes) return GPULET_EINVAL;
+    GroupNormArgs a;
+    const gpulet_status st = check_group_norm(d, a);
+    if (st == GPULET_OK) *bytes = group_norm_workspace(a);
+    return st;
+}
+
+extern "C" gpulet_status gpulet_group_norm(const gpulet_group_norm_desc *d, void *workspace, size_t workspace_bytes,
+                                           void *stream) {
+    GroupNormArgs a;
+    gpulet_status st = check_group_norm(d, a);
+    if (st != GPULET_OK) return st;
+    const size_t need = group_norm_workspace(a);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return GPULET_ENOMEM;
+        st = check_workspace(workspace, workspace_bytes);
+        if (st != GPULET_OK) return st;
+        const uint64_t all = 1ull * a.N * a.H * a.W, es = static_cast<uint64_t>(type_bytes(a.dtype));
+        const Rows ws = make_rows(workspace, 1, need, need);
+        if (meet(ws, make_rows(a.x, all, es * a.C, es * a.ldx)) || meet(ws, make_rows(a.residual, all, es * a.C, es * a.ldr)) ||
+            meet(ws, make_rows(a.y, all, es * a.C, es * a.ldy)) || meet(ws, make_rows(a.gamma, 1, 4ull * a.C, 4ull * a.C)) ||
+            meet(ws, make_rows(a.beta, 1, 4ull * a.C, 4ull * a.C)))
+            return GPULET_EINVAL;
+        a.ws = workspace;
+        a.ws_bytes = workspace_bytes;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    GPULET_HIP(launch_group_norm(a, stream_ctx(s), s));
+    return GPULET_OK;
+}
 
 extern "C" gpulet_status gpulet_conv2d_fwd_ex(const void *x, const void *w, const float *b, void *y,
                                               int N, int C, int H, int W, int K, int R, int S,

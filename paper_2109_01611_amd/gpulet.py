@@ -24,6 +24,8 @@ LIB_PATH = os.path.join(_HERE, "libgpulet.so")
 OK, EINVAL, EOVERSUB, EHIP, ENOMEM = 0, -1, -2, -3, -4
 POOL_MAX, POOL_AVG, POOL_GLOBAL_AVG = 0, 1, 2
 OP_CONV, OP_POOL, OP_FC, OP_DWCONV = 0, 1, 2, 3
+BF16, F16, F32 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 CONV_TILES = 15  # GPULET_CONV_TILES: set_conv_tile takes -1 .. CONV_TILES - 1
 
 
@@ -50,6 +52,19 @@ class ConvDesc(ctypes.Structure):
     _fields_ = [("x", c_void_p), ("w", c_void_p), ("b", c_void_p), ("y", c_void_p), ("residual", c_void_p)] + \
                [(n, c_int32) for n in ("N", "C", "H", "W", "K", "R", "S", "stride", "pad", "relu",
                                        "x_ch_stride", "x_ch_offset", "y_ch_stride", "y_ch_offset")]
+
+
+class MatmulDesc(ctypes.Structure):
+    """Mirror of ``gpulet_matmul_desc``."""
+    _fields_ = [(n, c_void_p) for n in ("x", "w", "b", "residual", "y")] + \
+               [(n, c_int32) for n in ("M", "N", "K", "ldx", "ldw", "ldr", "ldy", "dtype", "out_dtype", "act")]
+
+
+class GroupNormDesc(ctypes.Structure):
+    """Mirror of ``gpulet_group_norm_desc``."""
+    _fields_ = [(n, c_void_p) for n in ("x", "gamma", "beta", "residual", "y")] + \
+               [(n, c_int32) for n in ("N", "C", "H", "W", "groups", "x_ch_stride", "r_ch_stride", "y_ch_stride")] + \
+               [("eps", c_float), ("dtype", c_int32), ("act", c_int32)]
 
 
 class SchedModel(ctypes.Structure):
@@ -119,6 +134,10 @@ def _load():
         "gpulet_pool": ([P, P] + [I] * 8 + [P], c_int32),
         "gpulet_fc": ([P, P, P, P] + [I] * 5 + [P], c_int32),
         "gpulet_fc_static_scratch": ([P, P, P, P] + [I] * 5 + [P], c_int32),
+        "gpulet_matmul_workspace_bytes": ([POINTER(MatmulDesc), POINTER(c_size_t)], c_int32),
+        "gpulet_matmul": ([POINTER(MatmulDesc), P, c_size_t, P], c_int32),
+        "gpulet_group_norm_workspace_bytes": ([POINTER(GroupNormDesc), POINTER(c_size_t)], c_int32),
+        "gpulet_group_norm": ([POINTER(GroupNormDesc), P, c_size_t, P], c_int32),
         "gpulet_set_model_lanes": ([I], c_int32),
         "gpulet_model_schedule": ([POINTER(ModelDesc), I, I, IP, IP, IP, I, IP], c_int32),
         "gpulet_model_workspace_bytes": ([POINTER(ModelDesc), I, POINTER(c_size_t)], c_int32),
@@ -333,6 +352,43 @@ def fc(x, w, b, y, N, In, Out, relu, out_fp32=False, stream=None):
 def fc_static_scratch(x, w, b, y, N, In, Out, relu, out_fp32=False, stream=None):
     _check(lib.gpulet_fc_static_scratch(ptr(x), ptr(w), ptr(b), ptr(y), N, In, Out, int(relu), int(out_fp32),
                                         stream), "gpulet_fc_static_scratch")
+
+
+def matmul_desc(x, w, b, y, M, N, K, act=ACT_NONE, residual=None, ldx=0, ldw=0, ldr=0, ldy=0, dtype=BF16,
+                out_dtype=BF16):
+    """What ``matmul`` computes, made once and used for any number of calls.  Keeps references to the tensors."""
+    d = MatmulDesc(ptr(x), ptr(w), ptr(b), ptr(residual), ptr(y), M, N, K, ldx, ldw, ldr, ldy, dtype, out_dtype, act)
+    d._keep = (x, w, b, residual, y)
+    return d
+
+
+def matmul_workspace_bytes(desc):
+    n = c_size_t()
+    _check(lib.gpulet_matmul_workspace_bytes(byref(desc), byref(n)), "gpulet_matmul_workspace_bytes")
+    return n.value
+
+
+def matmul(desc, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib.gpulet_matmul(byref(desc), ptr(workspace), workspace_bytes, stream), "gpulet_matmul")
+
+
+def group_norm_desc(x, gamma, beta, y, N, C, H, W, groups, eps=1e-5, act=ACT_NONE, residual=None, x_ch_stride=0,
+                    r_ch_stride=0, y_ch_stride=0, dtype=BF16):
+    """What ``group_norm`` computes, made once and used for any number of calls.  Keeps references to the tensors."""
+    d = GroupNormDesc(ptr(x), ptr(gamma), ptr(beta), ptr(residual), ptr(y), N, C, H, W, groups, x_ch_stride, r_ch_stride,
+                      y_ch_stride, eps, dtype, act)
+    d._keep = (x, gamma, beta, residual, y)
+    return d
+
+
+def group_norm_workspace_bytes(desc):
+    n = c_size_t()
+    _check(lib.gpulet_group_norm_workspace_bytes(byref(desc), byref(n)), "gpulet_group_norm_workspace_bytes")
+    return n.value
+
+
+def group_norm(desc, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib.gpulet_group_norm(byref(desc), ptr(workspace), workspace_bytes, stream), "gpulet_group_norm")
 
 
 def time_conv2d(x, w, b, y, N, C, H, W, K, R, S, stride, pad, relu, residual=None, y_ch_stride=0,

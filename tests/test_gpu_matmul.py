@@ -1,0 +1,237 @@
+"""The matrix product with its epilogue against 64 bits: lengths from one to long, odd sizes, slices of wider rows, every
+type and activation, special values, streams and graphs.  Integer operands, whose sums are exact in fp32, are compared bit
+for bit."""
+
+import numpy as np
+import pytest
+import torch
+
+import block_reference as ref
+from paper_2109_01611_amd import gpulet
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, gpulet.BF16), "f16": (torch.float16, gpulet.F16), "f32": (torch.float32, gpulet.F32)}
+ACT = {"none": gpulet.ACT_NONE, "relu": gpulet.ACT_RELU, "silu": gpulet.ACT_SILU, "gelu": gpulet.ACT_GELU,
+       "gelu_tanh": gpulet.ACT_GELU_TANH}
+GUARD = -768.0    # exact in every type
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _workspace(size):
+    return torch.full((max(size, 1),), 0xFF, dtype=torch.uint8, device=DEV) if size else None    # NaNs, if anyone reads them
+
+
+class Case:
+    """Operands on the GPU inside guarded wider rows, starting `shift` elements in."""
+
+    def __init__(self, seed, M, N, K, dtype="bf16", out=None, act="none", bias=True, res=False, pad=(0, 0, 0, 0), shift=0,
+                 integers=False):
+        self.M, self.N, self.K, self.act = M, N, K, act
+        self.dtype, self.out = TYPES[dtype], TYPES[out or dtype]
+        g = torch.Generator().manual_seed(seed)
+
+        def draw(rows, cols, scale):
+            if integers:
+                return torch.randint(-4, 5, (rows, cols), generator=g).float()
+            return torch.randn(rows, cols, generator=g) * scale
+
+        def place(t, ld, dt):
+            flat = torch.full((t.shape[0] * ld + shift,), GUARD, dtype=dt, device=DEV)
+            view = flat[shift:].view(t.shape[0], ld)
+            view[:, :t.shape[1]] = t.to(DEV).to(dt)
+            return flat, view[:, :t.shape[1]]
+        self.ld = (K + pad[0], K + pad[1], N + pad[2], N + pad[3])
+        self.xf, self.x = place(draw(M, K, 1.0), self.ld[0], self.dtype[0])
+        self.wf, self.w = place(draw(N, K, K ** -0.5), self.ld[1], self.dtype[0])
+        self.b = draw(1, N, 0.5)[0].to(DEV) if bias else None
+        self.rf, self.r = place(draw(M, N, 1.0), self.ld[2], self.out[0]) if res else (None, None)
+        self.yf, self.y = place(torch.full((M, N), GUARD), self.ld[3], self.out[0])
+
+    def desc(self, y=None, **kw):
+        a = dict(x=self.x.data_ptr(), w=self.w.data_ptr(), b=self.b, y=(self.y if y is None else y).data_ptr(), M=self.M, N=self.N,
+                 K=self.K, act=ACT[self.act], residual=None if self.r is None else self.r.data_ptr(), ldx=self.ld[0],
+                 ldw=self.ld[1], ldr=self.ld[2], ldy=self.ld[3], dtype=self.dtype[1], out_dtype=self.out[1])
+        a.update(kw)
+        return gpulet.matmul_desc(**a)
+
+    def run(self, stream=None, workspace=True):
+        d = self.desc()
+        size = gpulet.matmul_workspace_bytes(d) if workspace else 0
+        ws = _workspace(size)
+        torch.cuda.synchronize()
+        gpulet.matmul(d, ws, size, stream)
+        torch.cuda.synchronize()
+        return self.y
+
+    def reference(self):
+        return ref.matmul(_np(self.x), _np(self.w), None if self.b is None else _np(self.b), None if self.r is None else _np(self.r),
+                          self.act)
+
+    def check(self, what=""):
+        y, err = self.reference()
+        ref.assert_within(_np(self.y), y, ref.rounded_bound(y, err, self.out[0], self.act), what)
+        self.check_guards()
+
+    def check_guards(self):
+        flat = self.yf.clone()
+        shift = flat.numel() - self.M * self.ld[3]
+        flat[shift:].view(self.M, self.ld[3])[:, :self.N] = GUARD
+        assert bool((flat == GUARD).all())
+
+
+SIZES = [(1, 1, 1), (1, 1, 8), (1, 64, 64), (2, 3, 5), (1, 1000, 2048), (1, 33, 4096), (3, 17, 1000), (4, 512, 72), (5, 128, 8200),
+         (8, 100, 520), (16, 16, 32), (17, 40, 96), (24, 1024, 512), (31, 65, 127), (33, 257, 264), (48, 96, 4104), (63, 64, 65),
+         (64, 64, 64), (65, 63, 1), (100, 300, 2056), (128, 128, 128), (129, 136, 200), (197, 320, 640), (255, 257, 33), (256, 256, 64),
+         (257, 512, 72), (300, 8, 1024), (520, 264, 96), (1000, 24, 40), (1024, 768, 256), (777, 1031, 129)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_integers_are_exact(size):
+    # |sum| <= 16 K + 8 < 2^24: fp32 holds every partial sum, in whatever order, and the result is one rounding of it
+    M, N, K = size
+    for dtype, out in (("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16")):
+        c = Case(1, M, N, K, dtype, out, res=True, integers=True)
+        want = (c.x.double().cpu() @ c.w.double().cpu().t() + c.b.double().cpu() + c.r.double().cpu()).to(c.out[0])
+        for workspace in (True, False):
+            c.y.fill_(GUARD)
+            assert torch.equal(c.run(workspace=workspace).cpu(), want), (dtype, out, workspace)
+            c.check_guards()
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")], ids="-".join)
+def test_types_and_activations(types, act):
+    for M, N, K, bias, res in ((1, 136, 264, True, False), (20, 72, 1032, False, True), (70, 130, 100, True, True),
+                               (300, 264, 192, True, True), (512, 512, 64, True, False)):
+        c = Case(2, M, N, K, types[0], types[1], act, bias, res)
+        c.run()
+        c.check((M, N, K))
+
+
+@pytest.mark.parametrize("size", [(1, 96, 520), (7, 40, 72), (40, 264, 136), (130, 136, 200), (600, 320, 136)], ids=str)
+@pytest.mark.parametrize("pad", [(8, 8, 8, 8), (1, 0, 0, 0), (0, 3, 0, 0), (0, 0, 5, 0), (0, 0, 0, 7), (64, 24, 2, 4)], ids=str)
+def test_slices_of_wider_rows(size, pad):
+    for shift in (0, 1, 4):
+        for out in ("bf16", "f32"):
+            c = Case(3, *size, dtype="bf16", out=out, act="silu", res=True, pad=pad, shift=shift)
+            c.run()
+            c.check((shift, out))
+
+
+def test_residual_in_place():
+    for size in ((1, 64, 128), (30, 1000, 4096), (200, 136, 2048), (700, 512, 512)):
+        a = Case(4, *size, res=True, act="relu")
+        a.run()
+        b = Case(4, *size, res=True, act="relu")
+        b.y, b.yf = b.r, b.rf
+        b.run()
+        assert torch.equal(a.y, b.y), size
+
+
+def test_same_call_same_bits_and_short_workspaces():
+    for size in ((2, 512, 4096), (40, 300, 8192), (180, 256, 4096)):
+        c = Case(5, *size, out="f32")
+        first = c.run().clone()
+        for _ in range(3):
+            assert torch.equal(c.run(), first)
+        d = c.desc()
+        full = gpulet.matmul_workspace_bytes(d)
+        for size_ in {0, 1, 255, 256, full // 2, max(full - 1, 0)}:
+            ws = _workspace(max(size_, 1))
+            c.y.fill_(GUARD)
+            torch.cuda.synchronize()
+            gpulet.matmul(d, ws, size_, None)
+            torch.cuda.synchronize()
+            c.check(size_)
+
+
+@pytest.mark.parametrize("size", [(1, 64, 256), (20, 40, 512), (100, 72, 1000), (300, 264, 192)], ids=str)
+def test_infinities_and_nan_stay_in_their_rows_and_columns(size):
+    M, N, K = size
+    c = Case(6, M, N, K, out="f32")
+    m, n = M - 1, N // 2
+    c.x[m, K - 1] = float("inf")
+    c.w[n, 0] = float("nan")
+    y = c.run().cpu()
+    clean = torch.ones(M, N, dtype=torch.bool)
+    clean[m] = False
+    clean[:, n] = False
+    assert bool(torch.isfinite(y[clean]).all())
+    assert bool(torch.isnan(y[:, n]).all())
+    row = torch.cat((y[m, :n], y[m, n + 1:]))
+    last = torch.cat((c.w[:n, K - 1], c.w[n + 1:, K - 1])).float().cpu()
+    want = torch.where(last == 0, torch.full_like(last, float("nan")), torch.sign(last) * float("inf"))
+    assert torch.equal(torch.isnan(row), torch.isnan(want)) and torch.equal(row[last != 0], want[last != 0])
+    c.check_guards()
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+def test_activations_at_the_ends(act):
+    # K = 1, x = 1: the value itself through the epilogue
+    v = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1.0, -1.0, 5.0, -5.0, 20.0, -20.0, 100.0, -100.0, 3e38, -3e38, float("inf"), float("nan")])
+    w = v.to(torch.bfloat16).view(-1, 1).to(DEV)
+    x = torch.ones(3, 1, dtype=torch.bfloat16, device=DEV)
+    y = torch.zeros(3, 16, device=DEV)
+    gpulet.matmul(gpulet.matmul_desc(x, w, None, y, 3, 16, 1, act=ACT[act], out_dtype=gpulet.F32))
+    torch.cuda.synchronize()
+    got = _np(y)
+    vb = _np(w)[:, 0]
+    with np.errstate(all="ignore"):
+        want = ref.activation(vb, act)
+    for i in range(3):
+        assert np.isnan(got[i, 15]) and got[i, 14] == np.inf
+        np.testing.assert_allclose(got[i, :14], want[:14], rtol=1e-5, atol=1e-6)
+
+
+def test_offsets_past_32_bits():
+    # 70 000 rows 2^16 elements apart: x spans 9.2 GB, y (dense) little; and the same for y
+    M, K, N, ld = 70000, 40, 24, 1 << 16
+    big = torch.empty(M * ld, dtype=torch.bfloat16, device=DEV)
+    x = big.view(M, ld)[:, :K]
+    x.copy_(torch.randint(-4, 5, (M, K), generator=torch.Generator(device=DEV).manual_seed(7), device=DEV).to(torch.bfloat16))
+    w = torch.randint(-4, 5, (N, K), generator=torch.Generator(device=DEV).manual_seed(8), device=DEV).to(torch.bfloat16)
+    y = torch.empty(M, N, device=DEV)
+    want = x.float() @ w.float().t()
+    gpulet.matmul(gpulet.matmul_desc(big, w, None, y, M, N, K, ldx=ld, out_dtype=gpulet.F32))
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    xd = x.contiguous()
+    gpulet.matmul(gpulet.matmul_desc(xd, w, None, big, M, N, K, ldy=ld))
+    torch.cuda.synchronize()
+    assert torch.equal(big.view(M, ld)[:, :N].float(), want)
+
+
+def test_gpu_lets_and_graphs():
+    shapes = ((1, 512, 4096), (24, 320, 2048), (150, 256, 4096), (600, 512, 640))
+    for pct in (25, 100):
+        with gpulet.Partition(0, pct, 0) as part:
+            for size in shapes:
+                c = Case(9, *size, act="gelu_tanh")
+                c.run(part.stream)
+                c.check((pct, size))
+    # two graphs with workspaces of their own, replayed between eager work on the same operands
+    cs = [Case(10 + i, *size, res=True, act="silu") for i, size in enumerate(shapes)]
+    for c in cs:
+        want = c.run().clone()
+        d = c.desc()
+        size = gpulet.matmul_workspace_bytes(d)
+        ws = [_workspace(size) for _ in range(2)]
+        graphs = []
+        for w in ws:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                gpulet.matmul(d, w, size, torch.cuda.current_stream().cuda_stream)
+            graphs.append(g)
+        for i in range(4):
+            c.y.fill_(GUARD)
+            graphs[i % 2].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.y, want)
+            c.x.mul_(-1)
+            c.run()
+            assert not torch.equal(c.y, want)
+            c.x.mul_(-1)
