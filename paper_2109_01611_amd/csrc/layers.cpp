@@ -87,7 +87,7 @@ gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a
     if (d->dtype < GPULET_BF16 || d->dtype > GPULET_F32 || d->act < GPULET_ACT_NONE || d->act > GPULET_ACT_GELU_TANH)
         return GPULET_EINVAL;
     if (!(d->eps >= 0.f) || d->eps > 3.0e38f) return GPULET_EINVAL;
-    if (1LL * d->N * d->groups > (1 << 22)) return GPULET_EINVAL;
+    if (1LL * d->N * d->groups > (1 << 21)) return GPULET_EINVAL;
     a = GroupNormArgs{d->x, d->gamma, d->beta, d->residual, d->y, d->N, d->C, d->H, d->W, d->groups,
                       d->x_ch_stride ? d->x_ch_stride : d->C, d->r_ch_stride ? d->r_ch_stride : d->C,
                       d->y_ch_stride ? d->y_ch_stride : d->C, d->dtype, d->act, d->eps, nullptr, 0};

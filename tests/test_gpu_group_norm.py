@@ -75,7 +75,7 @@ class Case:
 SIZES = [(1, 1, 1, 8, 8), (1, 1, 1, 64, 1), (3, 1, 1, 320, 32), (1, 1, 2, 6, 3), (2, 3, 5, 12, 4), (1, 7, 7, 2048, 32), (2, 8, 8, 1280, 32),
          (1, 8, 8, 30, 30), (5, 9, 11, 96, 32), (1, 16, 16, 640, 32), (1, 5, 3, 41, 1), (2, 37, 29, 82, 2), (3, 14, 14, 1024, 32),
          (1, 64, 64, 320, 32), (2, 56, 56, 64, 32), (1, 33, 31, 960, 32), (1, 64, 64, 24, 1), (1, 100, 100, 16, 16), (2, 50, 60, 136, 8),
-         (1, 128, 128, 128, 32), (1, 13, 17, 1536, 1), (1, 1, 4000, 48, 2), (40, 4, 4, 72, 8), (1, 200, 210, 33, 3), (1, 96, 96, 512, 1)]
+         (1, 128, 128, 128, 32), (2, 20, 17, 1031, 1), (1, 3, 300, 8208, 1), (1, 13, 17, 1536, 1), (1, 1, 4000, 48, 2), (40, 4, 4, 72, 8), (1, 200, 210, 33, 3), (1, 96, 96, 512, 1)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
