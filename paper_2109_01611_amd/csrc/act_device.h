@@ -11,7 +11,7 @@ namespace gpulet {
 
 constexpr float kLog2e = 1.44269504f;
 
-// v / (1 + exp(-s)): silu with s = v.  exp overflows to infinity below s = -88, where the quotient is zero.
+// v / (1 + exp(-s)).  exp overflows to infinity below s = -88, where the quotient is zero.
 __device__ __forceinline__ float gate(float v, float s) {
     return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * s));
 }
@@ -35,26 +35,31 @@ __device__ __forceinline__ float gelu(float v) {
     return v * (v > 0.f ? 1.f - q : q);
 }
 
-// v / 2 (1 + tanh(u)) = v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3).
-__device__ __forceinline__ float gelu_tanh(float v) {
-    return gate(v, 1.59576912f * (v + 0.044715f * (v * v * v)));
+// The activations are three pieces of code.  Kernels take the piece as a template argument: one that holds all three starts
+// later, since every line of its code comes from memory once.
+//   LINEAR  none, relu: v below 0 becomes 0 (NaN stays), or nothing does
+//   GATE    silu, gelu_tanh: v / (1 + exp(-s)) with s = v, or, as (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)),
+//           s = 2 sqrt(2 / pi) (v + 0.044715 v^3)
+//   NORMAL  gelu
+enum class ActCode { LINEAR, GATE, NORMAL };
+inline ActCode act_code(int act) {
+    return act == GPULET_ACT_GELU ? ActCode::NORMAL : act >= GPULET_ACT_SILU ? ActCode::GATE : ActCode::LINEAR;
 }
 
-// In place, on N values; `act` is the same for the whole wavefront.  ReLU keeps NaN.
-template <int N>
+// In place, on N values; `act` is one of the piece's and the same for the whole wavefront.
+template <ActCode A, int N>
 __device__ __forceinline__ void activate(float (&v)[N], int act) {
-    if (act == GPULET_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
-    } else if (act == GPULET_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = gate(v[i], v[i]);
-    } else if (act == GPULET_ACT_GELU) {
+    if constexpr (A == ActCode::NORMAL) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
-    } else if (act == GPULET_ACT_GELU_TANH) {
+    } else if constexpr (A == ActCode::GATE) {
+        const float k1 = act == GPULET_ACT_SILU ? 1.f : 1.59576912f, k3 = act == GPULET_ACT_SILU ? 0.f : 1.59576912f * 0.044715f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = gelu_tanh(v[i]);
+        for (int i = 0; i < N; ++i) v[i] = gate(v[i], v[i] * (k1 + k3 * (v[i] * v[i])));
+    } else {
+        const float lo = act == GPULET_ACT_RELU ? 0.f : -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < lo ? 0.f : v[i];
     }
 }
 

@@ -162,7 +162,7 @@ struct GroupNormArgs {
 };
 gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a);
 size_t group_norm_workspace(const GroupNormArgs &a);   // bytes launch_group_norm needs
-hipError_t launch_group_norm(const GroupNormArgs &a, const LaunchCtx &ctx, hipStream_t stream);
+hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream);
 
 // image_chain.hip: consecutive small layers, each reading what the one before wrote, as one launch with one
 // workgroup per image.  Every layer takes (C, H, W) to (K, P, Q) per image: convolutions with dense input and

@@ -5,10 +5,13 @@
 //
 // Bound by memory: x is read once and y written once, with about 20 vector operations an element.  Two forms:
 //
-// * held: a workgroup keeps whole groups of one image in registers: one launch, x read once.  For groups of up to
-//   kHeldBytes.
+// * held: a workgroup keeps whole groups of one image in registers: one launch, x read once.  For up to kHeldBytes.
 // * two launches for larger groups: the first reduces chunks of an image to (mean, sum of squared differences) per group,
-//   the second joins them and reads x again.
+//   the second joins them and reads x again, from the last-level cache where x fits there.  8 maps of 256x256x128 (134 MB)
+//   take 22 + 42 us, as much as 4.2 TB/s of the 268 MB that have to move; a copy of that size reaches 5.1.
+//
+// A single launch that holds what it read while all workgroups of an image exchange their sums would have to wait for
+// workgroups that may not be running: another launch of the same kind on another stream could hold their places.
 //
 // Which one runs depends on the shape of an image and the alignment of its rows only, not on how many images there are or
 // on the CUs of the gpu-let, so that an image's result has the same bits in any batch.
@@ -39,11 +42,14 @@ struct Params {
     int C, HW, G, cg;         // channels, pixels, groups, channels per group
     int ldx, ldr, ldy, act;
     float eps;
+    int threads;              // of a workgroup
     int gb, cb;               // groups and channels of a workgroup
     int upx, ug;              // units of V channels per pixel of a workgroup and per group
     int R, iters;             // pixels the threads cover at once, and how often (held)
+    int lanes;                // threads that join the values of a group: a power of two up to 64, all groups at once if it can
     int n_cb;                 // workgroups side by side in the channels
     int chunks, chunk;        // two launches: chunks of an image and their pixels
+    int stat_chunks, stat_chunk;   // normalising launch: the same of the launch before
     int total, per_die;       // workgroups, and a die's share of them
     FastDiv d_upx, d_ug, d_ncb, d_chunks;
 };
@@ -60,18 +66,22 @@ __device__ __forceinline__ Rsrc make_rsrc(const void *p, unsigned bytes) {
 }
 
 template <int UB>
-__device__ __forceinline__ typename RawUnit<UB>::Type load_unit(const Rsrc rs, unsigned off) {
-    if constexpr (UB == 2) return __builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0);
-    else if constexpr (UB == 4) return __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
-    else if constexpr (UB == 8) return __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
-    else return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+__device__ __forceinline__ typename RawUnit<UB>::Type load_unit(const Rsrc rs, unsigned off, unsigned soff = 0) {
+    if constexpr (UB == 2) return __builtin_amdgcn_raw_buffer_load_b16(rs, off, soff, 0);
+    else if constexpr (UB == 4) return __builtin_amdgcn_raw_buffer_load_b32(rs, off, soff, 0);
+    else if constexpr (UB == 8) return __builtin_amdgcn_raw_buffer_load_b64(rs, off, soff, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b128(rs, off, soff, 0);
 }
-template <int UB>
-__device__ __forceinline__ void store_unit(const Rsrc rs, unsigned off, typename RawUnit<UB>::Type v) {
-    if constexpr (UB == 2) __builtin_amdgcn_raw_buffer_store_b16(v, rs, off, 0, 0);
-    else if constexpr (UB == 4) __builtin_amdgcn_raw_buffer_store_b32(v, rs, off, 0, 0);
-    else if constexpr (UB == 8) __builtin_amdgcn_raw_buffer_store_b64(v, rs, off, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b128(v, rs, off, 0, 0);
+// NT: not to be kept in the caches.  The scalar part of the offset is added to the vector part: a 16-byte buffer store with a
+// scalar offset stored what the next vector instruction wrote to its first data register, in the last four of every 16
+// lanes.  The compiler keeps the two apart only where the store has no scalar offset.
+template <int UB, bool NT = false>
+__device__ __forceinline__ void store_unit(const Rsrc rs, unsigned off, unsigned soff, typename RawUnit<UB>::Type v) {
+    constexpr int AUX = NT ? 2 : 0;
+    if constexpr (UB == 2) __builtin_amdgcn_raw_buffer_store_b16(v, rs, off + soff, 0, AUX);
+    else if constexpr (UB == 4) __builtin_amdgcn_raw_buffer_store_b32(v, rs, off + soff, 0, AUX);
+    else if constexpr (UB == 8) __builtin_amdgcn_raw_buffer_store_b64(v, rs, off + soff, 0, AUX);
+    else __builtin_amdgcn_raw_buffer_store_b128(v, rs, off + soff, 0, AUX);
 }
 
 template <typename T, int V>
@@ -91,18 +101,25 @@ __device__ __forceinline__ typename RawUnit<V * sizeof(T)>::Type pack(const floa
     return u;
 }
 
-// Sum over a wavefront, the same in every lane: within rows of 16 lanes by DPP, then one lane of each row.
-__device__ __forceinline__ float wave_sum(float v) {
-    auto dpp = [](float f, auto ctrl) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f), decltype(ctrl)::value, 0xf, 0xf, true));
-    };
-    v += dpp(v, std::integral_constant<int, 0xB1>());    // lane ^ 1
-    v += dpp(v, std::integral_constant<int, 0x4E>());    // lane ^ 2
-    v += dpp(v, std::integral_constant<int, 0x141>());   // mirrored within 8
-    v += dpp(v, std::integral_constant<int, 0x140>());   // mirrored within 16
-    const int i = __float_as_int(v);
-    return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
-           (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));
+// The value of a lane of the other half among 2^(STEP + 1) lanes, once all lanes of each half agree (up to the order their
+// values were joined in): within rows of 16 lanes by DPP.
+template <int STEP>
+__device__ __forceinline__ float other_half(float f) {
+    if constexpr (STEP < 4) {
+        constexpr int CTRL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;   // lane ^ 1, lane ^ 2, mirrored within 8, 16
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f), CTRL, 0xf, 0xf, true));
+    } else {
+        return __shfl_xor(f, 1 << STEP);
+    }
+}
+
+// Sum over the first `lanes` (a power of two), the second, ... lanes of a wavefront.
+template <int STEP = 0>
+__device__ __forceinline__ float lane_sum(float v, int lanes) {
+    if ((1 << STEP) >= lanes) return v;
+    v += other_half<STEP>(v);
+    if constexpr (STEP < 5) return lane_sum<STEP + 1>(v, lanes);
+    return v;
 }
 
 // Sum of `v` over the threads of the calling thread's group; threads of no unit pass zero.  `part`: one float per thread
@@ -110,7 +127,7 @@ __device__ __forceinline__ float wave_sum(float v) {
 __device__ __forceinline__ float group_sum(float v, const Params &p, int my_group, float *part, float *res) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     if (p.gb == 1) {
-        v = wave_sum(v);
+        v = lane_sum(v, 64);
         if (lane == 0) res[wave] = v;
         __syncthreads();
         float s = 0.f;
@@ -119,14 +136,15 @@ __device__ __forceinline__ float group_sum(float v, const Params &p, int my_grou
     }
     part[threadIdx.x] = v;
     __syncthreads();
-    for (int g = wave; g < p.gb; g += waves) {
+    const int sub = threadIdx.x & (p.lanes - 1);
+    for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {
         float s = 0.f;
-        for (int i = lane; i < p.R * p.ug; i += 64) {
+        for (int i = sub; i < p.R * p.ug; i += p.lanes) {
             const int row = fdiv(i, p.d_ug);
             s += part[row * p.upx + g * p.ug + (i - row * p.ug)];
         }
-        s = wave_sum(s);
-        if (lane == 0) res[g] = s;
+        s = lane_sum(s, p.lanes);
+        if (sub == 0) res[g] = s;
     }
     __syncthreads();
     return res[my_group];
@@ -156,7 +174,7 @@ __device__ __forceinline__ void load_affine(const Params &p, int c, float (&a)[V
 }
 
 // One unit from raw to stored form.
-template <typename T, int V>
+template <typename T, int V, ActCode A>
 __device__ __forceinline__ typename RawUnit<V * sizeof(T)>::Type finish_unit(const typename RawUnit<V * sizeof(T)>::Type &x,
                                                                              const typename RawUnit<V * sizeof(T)>::Type &r, bool res,
                                                                              float mean, const float (&a)[V], const float (&b)[V],
@@ -171,12 +189,12 @@ __device__ __forceinline__ typename RawUnit<V * sizeof(T)>::Type finish_unit(con
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] += g[i];
     }
-    activate(f, act);
+    activate<A>(f, act);
     return pack<T, V>(f);
 }
 
 // Held: gb groups of one image in the registers of a workgroup, NR units a thread.
-template <typename T, int V, int NR>
+template <typename T, int V, int NR, ActCode A>
 __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
     constexpr int UB = V * static_cast<int>(sizeof(T));
     typedef typename RawUnit<UB>::Type Raw;
@@ -192,17 +210,23 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
                          (static_cast<unsigned>(p.HW - 1) * ld + p.cb) * static_cast<unsigned>(sizeof(T)));
     };
     const Rsrc xs = image(p.x, p.ldx), ys = image(p.y, p.ldy), rs = p.r ? image(p.r, p.ldr) : xs;
-    auto offset = [&](int i, int ld) {
-        const int q = at.row + i * p.R;
-        return at.in && q < p.HW ? static_cast<unsigned>(q * ld + at.c) * static_cast<unsigned>(sizeof(T)) : OOB;
-    };
+    // Rows of pixels before row `full` are whole: their offset is the thread's own plus a scalar; row `full` may be short.
+    const int full = p.iters - 1;
+    const bool tail = at.in && at.row + full * p.R < p.HW;
+    auto valid = [&](int i) { return i < full ? at.in : i == full && tail; };
+    auto base = [&](int ld) { return static_cast<unsigned>(at.row * ld + at.c) * static_cast<unsigned>(sizeof(T)); };
+    auto step = [&](int i, int ld) { return static_cast<unsigned>(min(i, full) * p.R * ld) * static_cast<unsigned>(sizeof(T)); };
     Raw xv[NR], rv[EARLY_RES ? NR : 1];
+    const unsigned xo = base(p.ldx), yo = base(p.ldy), ro = base(p.ldr);
 #pragma unroll
-    for (int i = 0; i < NR; ++i) xv[i] = load_unit<UB>(xs, offset(i, p.ldx));
+    for (int i = 0; i < NR; ++i) xv[i] = load_unit<UB>(xs, valid(i) ? xo : OOB, step(i, p.ldx));
     if (EARLY_RES && p.r) {
 #pragma unroll
-        for (int i = 0; i < (EARLY_RES ? NR : 1); ++i) rv[i] = load_unit<UB>(rs, offset(i, p.ldr));
+        for (int i = 0; i < (EARLY_RES ? NR : 1); ++i) rv[i] = load_unit<UB>(rs, valid(i) ? ro : OOB, step(i, p.ldr));
     }
+    // Sums are of differences from the group's first value: of a group of equal values the mean is that value, to the bit.
+    float first[1];
+    unpack<T, 1>(load_unit<sizeof(T)>(xs, static_cast<unsigned>(at.group * p.cg) * static_cast<unsigned>(sizeof(T))), first);
     float a[V], b[V];
     load_affine<V>(p, c0 + (at.in ? at.c : 0), a, b);
     const float inv = 1.f / (static_cast<float>(p.HW) * static_cast<float>(p.cg));
@@ -213,10 +237,10 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
         unpack<T, V>(xv[i], f);
         float t = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) t += f[j];
-        s += t;
+        for (int j = 0; j < V; ++j) t += f[j] - first[0];
+        s += valid(i) ? t : 0.f;
     }
-    const float mean = group_sum(s, p, at.group, part, res1) * inv;
+    const float mean = first[0] + group_sum(s, p, at.group, part, res1) * inv;
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
@@ -225,7 +249,7 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
         float t = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) t += (f[j] - mean) * (f[j] - mean);
-        s += at.in && at.row + i * p.R < p.HW ? t : 0.f;
+        s += valid(i) ? t : 0.f;
     }
     const float var = group_sum(s, p, at.group, part, res2) * inv;
     const float rstd = 1.f / __builtin_sqrtf(var + p.eps);
@@ -234,8 +258,8 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         Raw r{};
-        if (p.r) r = EARLY_RES ? rv[EARLY_RES ? i : 0] : load_unit<UB>(rs, offset(i, p.ldr));
-        store_unit<UB>(ys, offset(i, p.ldy), finish_unit<T, V>(xv[i], r, p.r != nullptr, mean, a, b, p.act));
+        if (p.r) r = EARLY_RES ? rv[EARLY_RES ? i : 0] : load_unit<UB>(rs, valid(i) ? ro : OOB, step(i, p.ldr));
+        store_unit<UB>(ys, valid(i) ? yo : OOB, step(i, p.ldy), finish_unit<T, V, A>(xv[i], r, p.r != nullptr, mean, a, b, p.act));
     }
 }
 
@@ -245,23 +269,59 @@ struct Stat {
 };
 __device__ __forceinline__ Stat join(const Stat a, const Stat b) {
     const float n = a.n + b.n;
-    const float f = n > 0.f ? b.n / n : 0.f;
+    const float f = a.n > 0.f ? b.n * __builtin_amdgcn_rcpf(n) : 1.f;   // equal means stay what they are, to the bit
     const float d = b.mean - a.mean;
     return Stat{n, a.mean + d * f, a.m2 + b.m2 + d * d * a.n * f};
 }
-__device__ __forceinline__ Stat join_lanes(Stat s, int width) {
-    for (int d = 1; d < width; d <<= 1) s = join(s, Stat{__shfl_xor(s.n, d), __shfl_xor(s.mean, d), __shfl_xor(s.m2, d)});
+template <int STEP = 0>
+__device__ __forceinline__ Stat join_lanes(Stat s, int lanes) {
+    if ((1 << STEP) >= lanes) return s;
+    s = join(s, Stat{other_half<STEP>(s.n), other_half<STEP>(s.mean), other_half<STEP>(s.m2)});
+    if constexpr (STEP < 5) return join_lanes<STEP + 1>(s, lanes);
     return s;
 }
 
-constexpr int kBatch = 8;   // units in flight a thread
+// Units in flight a thread in the two launches.  Twice as many are no faster (apply kernel of 5 images of 37 x 29 x 246 fp32
+// 4.6 us instead of 4.3) and make longer code.
+constexpr int batch_of(int unit_bytes) { return unit_bytes >= 8 ? 4 : 8; }
 
-// Statistics of one chunk of an image for the groups of a workgroup.  A thread takes kBatch units at a time: their mean and
-// squared differences from it, joined to what it has.
+// A thread's walk over the pixels of a chunk, batch_of(UB) units at a time: `full` batches without a test, then one with.
+template <typename T, int V>
+struct Walk {
+    static constexpr int UB = V * static_cast<int>(sizeof(T)), B = batch_of(UB);
+    typedef typename RawUnit<UB>::Type Raw;
+    int q, left;   // first pixel of the thread, pixels of the chunk from the first row on
+    const Place<V> &at;
+    const Params &p;
+    __device__ __forceinline__ Walk(const Params &p_, const Place<V> &at_, int q0, int q1) : q(q0 + at_.row), left(q1 - q0), at(at_), p(p_) {}
+    __device__ __forceinline__ bool full() const { return left >= B * p.R; }
+    __device__ __forceinline__ bool valid(int i) const { return at.in && at.row + i * p.R < left; }
+    __device__ __forceinline__ unsigned base(int ld) const {
+        return at.in ? static_cast<unsigned>(q * ld + at.c) * static_cast<unsigned>(sizeof(T)) : OOB;
+    }
+    __device__ __forceinline__ unsigned step(int ld) const { return static_cast<unsigned>(p.R * ld) * static_cast<unsigned>(sizeof(T)); }
+    __device__ __forceinline__ void load(const Rsrc rs, int ld, Raw (&v)[B]) const {
+        const unsigned o = base(ld), d = step(ld);
+        if (full()) {
+#pragma unroll
+            for (int i = 0; i < B; ++i) v[i] = load_unit<UB>(rs, o, i * d);
+        } else {
+#pragma unroll
+            for (int i = 0; i < B; ++i) v[i] = load_unit<UB>(rs, valid(i) ? o : OOB, i * d);
+        }
+    }
+    __device__ __forceinline__ void next() {
+        q += B * p.R;
+        left -= B * p.R;
+    }
+};
+
+// Statistics of one chunk of an image for the groups of a workgroup.  A thread sums differences from its first value and
+// their squares.  That value need not be near the mean: where it is D away, a fraction 1 / n of the thread's n values is,
+// the squared differences' sum is at least about D^2 and the roundings of n D^2 are n 2^-24 of it.
 template <typename T, int V>
 __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
-    constexpr int UB = V * static_cast<int>(sizeof(T));
-    typedef typename RawUnit<UB>::Type Raw;
+    typedef Walk<T, V> W;
     __shared__ float part[3][kMaxThreads];
     const int id = die_block(p.per_die, blockIdx.x);
     if (id >= p.total) return;
@@ -270,57 +330,60 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     const Place<V> at(p);
     const Rsrc xs = make_rsrc(static_cast<const char *>(p.x) + (static_cast<size_t>(n) * p.HW * p.ldx + c0) * sizeof(T),
                               (static_cast<unsigned>(p.HW - 1) * p.ldx + p.cb) * static_cast<unsigned>(sizeof(T)));
-    Stat s{0.f, 0.f, 0.f};
-    for (int q = q0 + at.row; q < q1 && at.in; q += kBatch * p.R) {
-        Raw xv[kBatch];
+    W w(p, at, q0, q1);
+    typename W::Raw xv[W::B];
+    w.load(xs, p.ldx, xv);
+    const float cnt = at.in && q0 + at.row < q1 ? static_cast<float>((q1 - q0 - at.row + p.R - 1) / p.R * V) : 0.f;
+    float first[V];
+    unpack<T, V>(xv[0], first);
+    const float k0 = first[0];
+    float sum = 0.f, sq = 0.f;
+    while (true) {
+        typename W::Raw cur[W::B];
+        const bool whole = w.full();
+        bool ok[W::B];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int qi = q + i * p.R;
-            xv[i] = load_unit<UB>(xs, qi < q1 ? static_cast<unsigned>(qi * p.ldx + at.c) * static_cast<unsigned>(sizeof(T)) : OOB);
+        for (int i = 0; i < W::B; ++i) {
+            cur[i] = xv[i];
+            ok[i] = whole || w.valid(i);
         }
-        float sum = 0.f, cnt = 0.f;
+        w.next();
+        const bool more = w.left > 0;
+        if (more) w.load(xs, p.ldx, xv);   // on its way while the batch before is summed
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            float f[V], u = 0.f;
-            unpack<T, V>(xv[i], f);
+        for (int i = 0; i < W::B; ++i) {
+            float f[V];
+            unpack<T, V>(cur[i], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) u += f[j];
-            sum += u;
-            cnt += q + i * p.R < q1 ? static_cast<float>(V) : 0.f;
+            for (int j = 0; j < V; ++j) {
+                const float d = ok[i] ? f[j] - k0 : 0.f;
+                sum += d;
+                sq += d * d;
+            }
         }
-        const float mean = sum / cnt;
-        float m2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            float f[V], u = 0.f;
-            unpack<T, V>(xv[i], f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) u += (f[j] - mean) * (f[j] - mean);
-            m2 += q + i * p.R < q1 ? u : 0.f;
-        }
-        s = join(s, Stat{cnt, mean, m2});
+        if (!more) break;
     }
-    part[0][threadIdx.x] = s.n;
-    part[1][threadIdx.x] = s.mean;
-    part[2][threadIdx.x] = s.m2;
+    const float shift = cnt > 0.f ? sum / cnt : 0.f;
+    part[0][threadIdx.x] = cnt;
+    part[1][threadIdx.x] = k0 + shift;
+    part[2][threadIdx.x] = fmaxf(sq - sum * shift, sq * 0.f);   // not below zero, and NaN where sq is not finite
     __syncthreads();
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    for (int g = wave; g < p.gb; g += waves) {
+    const int sub = threadIdx.x & (p.lanes - 1);
+    for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {
         Stat v{0.f, 0.f, 0.f};
-        for (int i = lane; i < p.R * p.ug; i += 64) {
+        for (int i = sub; i < p.R * p.ug; i += p.lanes) {
             const int row = fdiv(i, p.d_ug), j = row * p.upx + g * p.ug + (i - row * p.ug);
             v = join(v, Stat{part[0][j], part[1][j], part[2][j]});
         }
-        v = join_lanes(v, 64);
-        if (lane == 0) p.part[(static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.chunks + k] = make_float2(v.mean, v.m2);
+        v = join_lanes(v, p.lanes);
+        if (sub == 0) p.part[(static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.chunks + k] = make_float2(v.mean, v.m2);
     }
 }
 
 // Normalises one chunk of an image.
-template <typename T, int V>
+template <typename T, int V, bool NT, ActCode A>
 __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
-    constexpr int UB = V * static_cast<int>(sizeof(T));
-    typedef typename RawUnit<UB>::Type Raw;
+    typedef Walk<T, V> W;
     __shared__ float2 stat[kMaxGb];
     const int id = die_block(p.per_die, blockIdx.x);
     if (id >= p.total) return;
@@ -333,44 +396,45 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
                          (static_cast<unsigned>(p.HW - 1) * ld + p.cb) * static_cast<unsigned>(sizeof(T)));
     };
     const Rsrc xs = image(p.x, p.ldx), ys = image(p.y, p.ldy), rs = p.r ? image(p.r, p.ldr) : xs;
+    W w(p, at, q0, q1);
+    typename W::Raw xv[W::B], rv[W::B];
+    w.load(xs, p.ldx, xv);
+    if (p.r) w.load(rs, p.ldr, rv);
     float a[V], b[V];
     load_affine<V>(p, c0 + (at.in ? at.c : 0), a, b);
-    // sixteen lanes join the chunks of a group
-    for (int g = threadIdx.x >> 4; g < p.gb; g += blockDim.x >> 4) {
-        const float2 *q = p.part + (static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.chunks;
+    const int sub = threadIdx.x & (p.lanes - 1);
+    for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {
+        const float2 *q = p.part + (static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.stat_chunks;
         Stat v{0.f, 0.f, 0.f};
-        for (int i = threadIdx.x & 15; i < p.chunks; i += 16) {
+        for (int i = sub; i < p.stat_chunks; i += p.lanes) {
             const float2 e = q[i];
-            v = join(v, Stat{static_cast<float>((min(p.HW, (i + 1) * p.chunk) - i * p.chunk)) * static_cast<float>(p.cg), e.x, e.y});
+            const int first = i * p.stat_chunk;
+            v = join(v, Stat{static_cast<float>(min(p.HW - first, p.stat_chunk)) * static_cast<float>(p.cg), e.x, e.y});
         }
-        v = join_lanes(v, 16);
-        if ((threadIdx.x & 15) == 0) stat[g] = make_float2(v.mean, 1.f / __builtin_sqrtf(v.m2 / v.n + p.eps));
+        v = join_lanes(v, p.lanes);
+        if (sub == 0) stat[g] = make_float2(v.mean, 1.f / __builtin_sqrtf(v.m2 / v.n + p.eps));
     }
     __syncthreads();
-    if (!at.in) return;
     const float mean = stat[at.group].x, rstd = stat[at.group].y;
 #pragma unroll
     for (int j = 0; j < V; ++j) a[j] *= rstd;
-    for (int q = q0 + at.row; q < q1; q += kBatch * p.R) {
-        Raw xv[kBatch], rv[kBatch];
-        auto offset = [&](int i, int ld) {
-            const int qi = q + i * p.R;
-            return qi < q1 ? static_cast<unsigned>(qi * ld + at.c) * static_cast<unsigned>(sizeof(T)) : OOB;
-        };
+    while (true) {
+        const unsigned o = w.base(p.ldy), d = w.step(p.ldy);
+        const bool whole = w.full() && at.in;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) xv[i] = load_unit<UB>(xs, offset(i, p.ldx));
-        if (p.r) {
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) rv[i] = load_unit<UB>(rs, offset(i, p.ldr));
+        for (int i = 0; i < W::B; ++i) {
+            const typename W::Raw y = finish_unit<T, V, A>(xv[i], p.r ? rv[i] : xv[i], p.r != nullptr, mean, a, b, p.act);
+            store_unit<W::UB, NT>(ys, whole || w.valid(i) ? o : OOB, i * d, y);
         }
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-            store_unit<UB>(ys, offset(i, p.ldy), finish_unit<T, V>(xv[i], p.r ? rv[i] : xv[i], p.r != nullptr, mean, a, b, p.act));
+        w.next();
+        if (w.left <= 0) break;
+        w.load(xs, p.ldx, xv);
+        if (p.r) w.load(rs, p.ldr, rv);
     }
 }
 
 // One workgroup per image and group, element by element: groups of more than kMaxThreads units.
-template <typename T>
+template <typename T, ActCode A>
 __global__ __launch_bounds__(kMaxThreads) void wide_kernel(Params p) {
     __shared__ float res1[kMaxGb], res2[kMaxGb];
     const int n = fdiv(blockIdx.x, p.d_ncb), g = blockIdx.x - n * p.n_cb;
@@ -379,6 +443,7 @@ __global__ __launch_bounds__(kMaxThreads) void wide_kernel(Params p) {
     const T *r = p.r ? static_cast<const T *>(p.r) + px * p.ldr + g * p.cg : nullptr;
     T *y = static_cast<T *>(p.y) + px * p.ldy + g * p.cg;
     const float inv = 1.f / (static_cast<float>(p.HW) * static_cast<float>(p.cg));
+    const float first = static_cast<float>(x[0]);
     float mean = 0.f, rstd = 0.f;
     for (int pass = 0; pass < 3; ++pass) {
         float s = 0.f, t = 0.f;
@@ -386,13 +451,13 @@ __global__ __launch_bounds__(kMaxThreads) void wide_kernel(Params p) {
             for (int c = threadIdx.x; c < p.cg; c += kMaxThreads) {
                 float v[1] = {static_cast<float>(x[q * p.ldx + c])};
                 if (pass == 0) {
-                    t += v[0];
+                    t += v[0] - first;
                 } else if (pass == 1) {
                     t += (v[0] - mean) * (v[0] - mean);
                 } else {
                     v[0] = (v[0] - mean) * (p.gamma ? rstd * p.gamma[g * p.cg + c] : rstd) + (p.beta ? p.beta[g * p.cg + c] : 0.f);
                     if (r) v[0] += static_cast<float>(r[q * p.ldr + c]);
-                    activate(v, p.act);
+                    activate<A>(v, p.act);
                     y[q * p.ldy + c] = static_cast<T>(v[0]);
                 }
             }
@@ -402,39 +467,65 @@ __global__ __launch_bounds__(kMaxThreads) void wide_kernel(Params p) {
             }
         }
         s += t;
-        if (pass == 0) mean = group_sum(s, p, 0, nullptr, res1) * inv;
+        if (pass == 0) mean = first + group_sum(s, p, 0, nullptr, res1) * inv;
         else if (pass == 1) rstd = 1.f / __builtin_sqrtf(group_sum(s, p, 0, nullptr, res2) * inv + p.eps);
     }
 }
 
 // ---- host side
 
-constexpr size_t kHeldBytes = 96 << 10;   // of a group: see DESIGN
-constexpr int kHeldDwords = 40;           // registers of a thread that hold units
-constexpr size_t kChunkBytes = 128 << 10;
-constexpr int kMaxChunks = 64;
+// Bytes of the groups a workgroup holds, at most.  Above, too few workgroups read pieces of pixels too short for the memory
+// system: held and in two launches took, bf16, 32 groups,
+//    5 KB  8x8x1280   1 image  4.3 and 7.7 us    32 images  7.8 and 10.5
+//   12 KB  14x14x1024 1 image  4.6 and 7.4       32 images 11.1 and 15.3
+//   20 KB  16x16x1280 1 image  7.5 and 7.6       32 images 21.6 and 21.0
+//   49 KB  28x28x256  1 image 11.0 and 7.5       32 images 13.5 and 15.0
+//   80 KB  32x32x1280 1 image 11.8 and 8.2       32 images 62   and 51
+constexpr size_t kHeldBytes = 32 << 10;
+constexpr int kHeldDwords = 24;           // registers of a thread that hold units
+// Bytes of a workgroup's chunk.  Statistics: 32 chunks (one for each lane that joins them), unless they are out of these
+// limits.  Normalising: an image is spread over 256 workgroups within these limits.
+constexpr size_t kMinStats = 8 << 10, kMaxStats = 256 << 10, kMinApply = 8 << 10, kMaxApply = 32 << 10;
+// Results of this size and more are stored past the caches: they would push out the x that is still to be read a second
+// time, and most of them would be gone from the caches before anybody reads them.
+constexpr size_t kStreamBytes = 64 << 20;
 
 struct Plan {
     enum Form { HELD, TWO, WIDE } form;
-    int V, threads, iters;
-    Params p;
+    int V, iters;
+    bool stream_out;
+    Params p, q;   // of the only or first launch, and of the second
 };
 
-void set_blocks(Plan &pl, int N, int per_image) {
-    pl.p.total = N * per_image;
-    pl.p.per_die = (pl.p.total + 7) / 8;
+void set_blocks(Params &p, int N, int per_image) {
+    p.total = N * per_image;
+    p.per_die = (p.total + 7) / 8;
 }
 
 void set_units(Params &p, int V, int gb, int threads) {
+    p.threads = threads;
     p.gb = gb;
     p.cb = gb * p.cg;
     p.upx = p.cb / V;
     p.ug = p.cg / V;
     p.R = threads / p.upx;
+    p.lanes = 64;
+    while (p.lanes > 1 && p.lanes * gb > threads) p.lanes /= 2;
     p.n_cb = p.G / gb;
     p.d_upx = make_fastdiv(p.upx);
     p.d_ug = make_fastdiv(p.ug);
     p.d_ncb = make_fastdiv(p.n_cb);
+}
+
+// Chunks of about `piece` bytes, made of whole batches.
+void set_chunks(Params &p, int V, int unit_bytes, int gb, int threads, size_t block_bytes, size_t piece, int N) {
+    set_units(p, V, gb, threads);
+    const int chunks = static_cast<int>(std::max<size_t>(1, block_bytes / piece));
+    const int whole = p.R * batch_of(unit_bytes);
+    p.chunk = ((p.HW + chunks - 1) / chunks + whole - 1) / whole * whole;
+    p.chunks = (p.HW + p.chunk - 1) / p.chunk;
+    p.d_chunks = make_fastdiv(p.chunks);
+    set_blocks(p, N, p.n_cb * p.chunks);
 }
 
 Plan make_plan(const GroupNormArgs &a) {
@@ -457,8 +548,7 @@ Plan make_plan(const GroupNormArgs &a) {
     if (p.cg / V > kMaxThreads) {
         pl.form = Plan::WIDE;
         set_units(p, p.cg, 1, 1);
-        pl.threads = kMaxThreads;
-        set_blocks(pl, a.N, p.G);
+        set_blocks(p, a.N, p.G);
         return pl;
     }
     const int unit_dwords = std::max(1, V * es / 4);
@@ -469,85 +559,93 @@ Plan make_plan(const GroupNormArgs &a) {
         do ++gb; while (p.G % gb != 0);
     }
     if (gb > kMaxGb) gb = 1;
-    if (group_bytes <= kHeldBytes) {
-        for (int g = gb; g >= 1; --g) {
-            if (p.G % g != 0 || g * p.cg / V > kMaxThreads) continue;
-            // the fewest threads that hold the groups in two dwords' worth of 16-byte units each, or else as few as possible
-            for (int threads = 64; threads <= kMaxThreads; threads *= 2) {
-                const int upx = g * p.cg / V;
-                if (upx > threads) continue;
-                const int iters = (p.HW + threads / upx - 1) / (threads / upx);
-                if (iters * unit_dwords > (threads < kMaxThreads ? 8 : kHeldDwords)) continue;
-                pl.form = Plan::HELD;
-                pl.threads = threads;
-                pl.iters = iters;
-                set_units(p, V, g, threads);
-                set_blocks(pl, a.N, p.n_cb);
-                return pl;
-            }
+    if (group_bytes * gb <= kHeldBytes && gb * p.cg / V <= kMaxThreads) {
+        // the fewest threads that hold the groups in 8 dwords each, or else as few dwords as possible
+        const int upx = gb * p.cg / V;
+        for (int threads = 64; threads <= kMaxThreads; threads *= 2) {
+            if (upx > threads) continue;
+            const int rows = threads / upx, iters = (p.HW + rows - 1) / rows;
+            if (iters * unit_dwords > (threads < kMaxThreads ? 8 : kHeldDwords)) continue;
+            pl.form = Plan::HELD;
+            pl.iters = p.iters = iters;
+            set_units(p, V, gb, threads);
+            set_blocks(p, a.N, p.n_cb);
+            return pl;
         }
     }
     pl.form = Plan::TWO;
-    // a pixel's piece of 256 bytes, or all of a group
+    // a pixel's piece of 128 bytes, a line, or all of a group
     gb = 1;
-    while (gb < p.G && gb * p.cg * es < 256) {
+    while (gb < p.G && gb * p.cg * es < 128) {
         int next = gb + 1;
         while (p.G % next != 0) ++next;
         if (next > kMaxGb || next * p.cg / V > kMaxThreads) break;
         gb = next;
     }
-    pl.threads = std::max(256, (gb * p.cg / V + 63) / 64 * 64);
-    set_units(p, V, gb, pl.threads);
-    const size_t bytes = static_cast<size_t>(p.HW) * p.cb * es;
-    const int chunks = static_cast<int>(std::min<size_t>(kMaxChunks, std::max<size_t>(1, bytes / kChunkBytes)));
-    p.chunk = (p.HW + chunks - 1) / chunks;
-    p.chunks = (p.HW + p.chunk - 1) / p.chunk;
-    p.d_chunks = make_fastdiv(p.chunks);
-    set_blocks(pl, a.N, p.n_cb * p.chunks);
+    const size_t block_bytes = static_cast<size_t>(p.HW) * gb * p.cg * es;
+    const size_t stats = std::min(kMaxStats, std::max(kMinStats, block_bytes / 32));
+    const size_t apply = std::min(kMaxApply, std::max(kMinApply, block_bytes * (p.G / gb) / 256));
+    pl.stream_out = static_cast<size_t>(a.N) * p.HW * p.C * es >= kStreamBytes;
+    pl.q = p;
+    const int fewest = (gb * p.cg / V + 63) / 64 * 64;   // threads of one row
+    set_chunks(p, V, V * es, gb, std::max(stats >= (64 << 10) ? 512 : 256, fewest), block_bytes, stats, a.N);
+    set_chunks(pl.q, V, V * es, gb, std::max(256, fewest), block_bytes, apply, a.N);
+    pl.q.stat_chunks = p.chunks;
+    pl.q.stat_chunk = p.chunk;
     return pl;
 }
 
-template <typename T, int V>
+template <typename T, int V, ActCode A>
 hipError_t launch_units(const Plan &pl, hipStream_t stream) {
-    const dim3 grid(8 * pl.p.per_die), block(pl.threads);
+    const dim3 grid(8 * pl.p.per_die), block(pl.p.threads);
     constexpr int UD = V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1;   // dwords of a unit
     if (pl.form == Plan::HELD) {
-        if (pl.iters * UD <= 8) held_kernel<T, V, 8 / UD><<<grid, block, 0, stream>>>(pl.p);
-        else if (pl.iters * UD <= 20) held_kernel<T, V, 20 / UD><<<grid, block, 0, stream>>>(pl.p);
-        else held_kernel<T, V, kHeldDwords / UD><<<grid, block, 0, stream>>>(pl.p);
+        if (pl.iters * UD <= 8) held_kernel<T, V, 8 / UD, A><<<grid, block, 0, stream>>>(pl.p);
+        else held_kernel<T, V, kHeldDwords / UD, A><<<grid, block, 0, stream>>>(pl.p);
         return hipGetLastError();
     }
     stats_kernel<T, V><<<grid, block, 0, stream>>>(pl.p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    apply_kernel<T, V><<<grid, block, 0, stream>>>(pl.p);
+    const dim3 grid2(8 * pl.q.per_die), block2(pl.q.threads);
+    if (pl.stream_out) apply_kernel<T, V, true, A><<<grid2, block2, 0, stream>>>(pl.q);
+    else apply_kernel<T, V, false, A><<<grid2, block2, 0, stream>>>(pl.q);
     return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, ActCode A>
 hipError_t launch_type(const Plan &pl, hipStream_t stream) {
     if (pl.form == Plan::WIDE) {
-        wide_kernel<T><<<dim3(pl.p.total), kMaxThreads, 0, stream>>>(pl.p);
+        wide_kernel<T, A><<<dim3(pl.p.total), kMaxThreads, 0, stream>>>(pl.p);
         return hipGetLastError();
     }
     switch (pl.V) {
         case 8:
-            if constexpr (sizeof(T) == 2) return launch_units<T, 8>(pl, stream);
+            if constexpr (sizeof(T) == 2) return launch_units<T, 8, A>(pl, stream);
             return hipErrorInvalidValue;
-        case 4: return launch_units<T, 4>(pl, stream);
-        case 2: return launch_units<T, 2>(pl, stream);
-        default: return launch_units<T, 1>(pl, stream);
+        case 4: return launch_units<T, 4, A>(pl, stream);
+        case 2: return launch_units<T, 2, A>(pl, stream);
+        default: return launch_units<T, 1, A>(pl, stream);
+    }
+}
+
+template <typename T>
+hipError_t launch_act(const Plan &pl, hipStream_t stream) {
+    switch (act_code(pl.p.act)) {
+        case ActCode::NORMAL: return launch_type<T, ActCode::NORMAL>(pl, stream);
+        case ActCode::GATE: return launch_type<T, ActCode::GATE>(pl, stream);
+        default: return launch_type<T, ActCode::LINEAR>(pl, stream);
     }
 }
 
 }  // namespace
 
-hipError_t launch_group_norm(const GroupNormArgs &a, const LaunchCtx &ctx, hipStream_t stream) {
+hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream) {
     Plan pl = make_plan(a);
-    pl.p.part = static_cast<float2 *>(a.ws);
-    if (a.dtype == GPULET_BF16) return launch_type<__bf16>(pl, stream);
-    if (a.dtype == GPULET_F16) return launch_type<_Float16>(pl, stream);
-    return launch_type<float>(pl, stream);
+    pl.p.part = pl.q.part = static_cast<float2 *>(a.ws);
+    if (a.dtype == GPULET_BF16) return launch_act<__bf16>(pl, stream);
+    if (a.dtype == GPULET_F16) return launch_act<_Float16>(pl, stream);
+    return launch_act<float>(pl, stream);
 }
 
 size_t group_norm_workspace(const GroupNormArgs &a) {

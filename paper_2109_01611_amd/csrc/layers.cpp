@@ -166,7 +166,7 @@ extern "C" gpulet_status gpulet_group_norm(const gpulet_group_norm_desc *d, void
         a.ws_bytes = workspace_bytes;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    GPULET_HIP(launch_group_norm(a, stream_ctx(s), s));
+    GPULET_HIP(launch_group_norm(a, s));
     return GPULET_OK;
 }
 

@@ -37,7 +37,7 @@ struct Params {
 };
 
 // bias, residual and activation on N consecutive columns of row m, then the store.
-template <int N, typename T>
+template <int N, typename T, ActCode A>
 __device__ __forceinline__ void finish(const Params &p, int m, int n, float (&v)[N]) {
     const T *r = p.r ? static_cast<const T *>(p.r) + static_cast<long long>(m) * p.ldr + n : nullptr;
     T *y = static_cast<T *>(p.y) + static_cast<long long>(m) * p.ldy + n;
@@ -47,7 +47,7 @@ __device__ __forceinline__ void finish(const Params &p, int m, int n, float (&v)
         if (p.b) v[i] += p.b[n + i];
         if (r) v[i] += static_cast<float>(r[i]);
     }
-    activate(v, p.act);
+    activate<A>(v, p.act);
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (n + i < p.N) y[i] = static_cast<T>(v[i]);
@@ -71,7 +71,7 @@ __device__ __forceinline__ uint4 load8(const T *row, int k, int K, bool row_ok) 
 
 // A tile of 64 rows by 64 columns a workgroup, four wavefronts of 32 x 32, one slice of 64 elements of the depth at a time
 // through LDS, the next one on its way into registers meanwhile.  Takes any alignment and any depth.
-template <typename T, typename TO>
+template <typename T, typename TO, ActCode A>
 __global__ __launch_bounds__(256) void matmul_any_kernel(Params p) {
     __shared__ uint4 tile[2][64 * 8];   // x and w: 64 rows of 8 chunks of 8 elements
     const int tm = fdiv(blockIdx.x, p.d_tiles_n), tn = blockIdx.x - tm * p.tiles_n;
@@ -131,13 +131,18 @@ __global__ __launch_bounds__(256) void matmul_any_kernel(Params p) {
         for (int j = 0; j < 2; ++j) {
             const int m = m0 + wm + 16 * i + (lane & 15), n = n0 + wn + 16 * j + 4 * (lane >> 4);
             float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (m < p.M && n < p.N) finish<4, TO>(p, m, n, v);
+            if (m < p.M && n < p.N) finish<4, TO, A>(p, m, n, v);
         }
 }
 
 template <typename T, typename TO>
 hipError_t launch_any(const Params &p, int tiles_m, hipStream_t stream) {
-    matmul_any_kernel<T, TO><<<dim3(tiles_m * p.tiles_n), 256, 0, stream>>>(p);
+    const dim3 grid(tiles_m * p.tiles_n);
+    switch (act_code(p.act)) {
+        case ActCode::NORMAL: matmul_any_kernel<T, TO, ActCode::NORMAL><<<grid, 256, 0, stream>>>(p); break;
+        case ActCode::GATE: matmul_any_kernel<T, TO, ActCode::GATE><<<grid, 256, 0, stream>>>(p); break;
+        default: matmul_any_kernel<T, TO, ActCode::LINEAR><<<grid, 256, 0, stream>>>(p);
+    }
     return hipGetLastError();
 }
 

@@ -126,15 +126,16 @@ def test_large_means_keep_the_variance():
 
 
 def test_constant_groups():
-    for size in ((1, 4, 4, 64, 8), (1, 90, 90, 64, 2)):
+    for size in ((1, 4, 4, 64, 8), (1, 3, 9, 30, 3), (2, 7, 5, 24, 8), (1, 90, 90, 64, 2), (1, 1, 3, 8200, 1)):
         c = Case(6, *size, act="relu", res=True)
-        c.x.fill_(3.0)
-        c.run()
-        c.check(size)
+        c.x.fill_(3.3)
+        want = torch.relu(c.beta + c.r.float()).to(torch.bfloat16)
+        assert torch.equal(c.run(), want), size
         c = Case(6, *size, eps=0.0)
-        c.x[..., :size[3] // size[4]] = 3.0
+        c.x[..., :size[3] // size[4]] = 3.3
         y = c.run()
-        assert bool(torch.isnan(y[..., :size[3] // size[4]]).all()) and bool(torch.isfinite(y[..., size[3] // size[4]:]).all())
+        cg = size[3] // size[4]
+        assert bool(torch.isnan(y[..., :cg]).all()) and bool(torch.isfinite(y[..., cg:]).all())
 
 
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
