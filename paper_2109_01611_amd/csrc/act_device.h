@@ -55,7 +55,7 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
     } else if constexpr (A == ActCode::GATE) {
         const float k1 = act == GPULET_ACT_SILU ? 1.f : 1.59576912f, k3 = act == GPULET_ACT_SILU ? 0.f : 1.59576912f * 0.044715f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = gate(v[i], v[i] * (k1 + k3 * (v[i] * v[i])));
+        for (int i = 0; i < N; ++i) v[i] = gate(v[i], v[i] * (k1 + k3 * __builtin_fminf(v[i] * v[i], 1e30f)));   // 0 * inf is no number
     } else {
         const float lo = act == GPULET_ACT_RELU ? 0.f : -__builtin_inff();
 #pragma unroll

@@ -2,6 +2,18 @@
 //   y[m, n] = act(sum_k x[m, k] w[n, k] + b[n] + r[m, n])
 // for the per-pixel and per-row layers of a forward pass (paper Sec. 5) that a ReLU convolution or the fully connected
 // layer cannot stand for: wide activations, fp16, fp32 results, rows that are slices of wider ones, any number of rows.
+//
+// Forms, chosen per call by an estimate of their times (choose_form):
+//   direct   few rows or few tiles: operands go from memory straight into the matrix instructions, the depth is shared by
+//            the wavefronts of a workgroup.  Bound by memory: 1 x 4096 x 4096 8.3 us (4.0 TB/s of the weights).
+//   tile     64x64, 128x64 and 128x128 tiles, operands staged in LDS by transfers that pass no register.  Bound by the
+//            rate at which a CU takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128
+//            56 us, 933 TFLOP/s.  The 64x64 and 128x128 ones also with a depth that up to eight workgroups share, whose
+//            sums meet in the workspace.
+//   big      256x256 tiles, 160 KB of LDS: as many matrix instructions as transfers can feed.  8192 x 4096 x 4096 216 us,
+//            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 1.33.
+//   staged   64x64 tiles whose operands pass through registers: rows that do not start at multiples of 16 bytes.
+//            2048 x 1024 x 1001 19 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,36 +44,98 @@ struct Params {
     const void *r;
     void *y;
     int M, N, K, ldx, ldw, ldr, ldy, act;
-    int tiles_n;
-    FastDiv d_tiles_n;
+    int tiles_m, tiles_n;
+    int total, per_die;     // workgroups, and a die's share of them
+    int splits;             // workgroups that share a tile
+    int slices;             // slices of the depth: of 64, a workgroup's (splits > 1); of 32, a wavefront's (direct)
+    float *part;            // splits > 1: [split][M][N] sums
+    int vec;                // rows of y and the residual allow 16-byte accesses
+    FastDiv d_tiles, d_tiles_n, d_tiles_m;
 };
 
-// bias, residual and activation on N consecutive columns of row m, then the store.
-template <int N, typename T, ActCode A>
-__device__ __forceinline__ void finish(const Params &p, int m, int n, float (&v)[N]) {
+template <int N> struct Bytes;
+template <> struct Bytes<8> { typedef uint2 Type; };
+template <> struct Bytes<16> { typedef uint4 Type; };
+
+// bias, residual and activation on NC consecutive columns of row m, then the store; `full`: all of them exist and can be
+// reached 16 bytes at a time.  `bias` holds the columns' bias.
+template <int NC, typename T, ActCode A>
+__device__ __forceinline__ void finish(const Params &p, int m, int n, bool full, const float (&bias)[NC], float (&v)[NC]) {
     const T *r = p.r ? static_cast<const T *>(p.r) + static_cast<long long>(m) * p.ldr + n : nullptr;
     T *y = static_cast<T *>(p.y) + static_cast<long long>(m) * p.ldy + n;
+    typedef typename Bytes<NC * sizeof(T) < 16 ? 8 : 16>::Type Raw;
+    constexpr int PER = sizeof(Raw) / sizeof(T);   // elements of an access
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if (n + i >= p.N) break;
-        if (p.b) v[i] += p.b[n + i];
-        if (r) v[i] += static_cast<float>(r[i]);
+    for (int i = 0; i < NC; ++i) v[i] += bias[i];
+    if (NC % PER == 0 && full) {
+        if (r) {
+#pragma unroll
+            for (int i = 0; i < NC; i += PER) {
+                T e[PER];
+                const Raw u = *reinterpret_cast<const Raw *>(r + i);
+                __builtin_memcpy(e, &u, sizeof(u));
+#pragma unroll
+                for (int j = 0; j < PER; ++j) v[i + j] += static_cast<float>(e[j]);
+            }
+        }
+        activate<A>(v, p.act);
+#pragma unroll
+        for (int i = 0; i < NC; i += PER) {
+            T e[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) e[j] = static_cast<T>(v[i + j]);
+            Raw u;
+            __builtin_memcpy(&u, e, sizeof(u));
+            *reinterpret_cast<Raw *>(y + i) = u;
+        }
+        return;
+    }
+    if (r) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            if (n + i < p.N) v[i] += static_cast<float>(r[i]);
     }
     activate<A>(v, p.act);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < NC; ++i)
         if (n + i < p.N) y[i] = static_cast<T>(v[i]);
 }
 
-// Elements [k, k + 8) of a row; zero past its end.  Rows may start at any element.
-template <typename T>
-__device__ __forceinline__ uint4 load8(const T *row, int k, int K, bool row_ok) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (!row_ok || k >= K) return v;
-    if (k + 8 <= K) {
+template <int NC>
+__device__ __forceinline__ void load_bias(const Params &p, int n, float (&b)[NC]) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) b[i] = p.b && n + i < p.N ? p.b[n + i] : 0.f;
+}
+
+// Elements [k, k + 8) of a row, all of them in it.  ODD: the row may start at any element; a load that is not aligned to 4
+// bytes takes several times as long (787 x 333 x 1001 18.5 us, x 1002 8.0), so 20 bytes from the 4-byte boundary before are
+// loaded and shifted.  The first and the last 2 bytes then belong to no element of the eight; they lie in the same aligned 4
+// bytes as one that does.
+template <bool ODD, typename T>
+__device__ __forceinline__ uint4 load_whole(const T *row, int k) {
+    uint4 v;
+    if constexpr (ODD) {
+        const unsigned long long at = reinterpret_cast<unsigned long long>(row + k);
+        const unsigned shift = (static_cast<unsigned>(at) & 2u) * 8u;
+        const unsigned *q = reinterpret_cast<const unsigned *>(at & ~3ull);
+        __builtin_memcpy(&v, q, 16);
+        const unsigned last = q[shift ? 4 : 3];
+        v.x = __builtin_amdgcn_alignbit(v.y, v.x, shift);
+        v.y = __builtin_amdgcn_alignbit(v.z, v.y, shift);
+        v.z = __builtin_amdgcn_alignbit(v.w, v.z, shift);
+        v.w = __builtin_amdgcn_alignbit(last, v.w, shift);
+    } else {
         __builtin_memcpy(&v, row + k, 16);
-        return v;
     }
+    return v;
+}
+
+// Elements [k, k + 8) of a row; zero from K on.
+template <bool ODD, typename T>
+__device__ __forceinline__ uint4 load_cut(const T *row, int k, int K) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (k + 8 <= K) return load_whole<ODD>(row, k);
+    if (k >= K) return v;
     unsigned short e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = k + i < K ? reinterpret_cast<const unsigned short *>(row)[k + i] : 0;
@@ -69,10 +143,12 @@ __device__ __forceinline__ uint4 load8(const T *row, int k, int K, bool row_ok) 
     return v;
 }
 
+// ---- rows that start anywhere
+
 // A tile of 64 rows by 64 columns a workgroup, four wavefronts of 32 x 32, one slice of 64 elements of the depth at a time
-// through LDS, the next one on its way into registers meanwhile.  Takes any alignment and any depth.
-template <typename T, typename TO, ActCode A>
-__global__ __launch_bounds__(256) void matmul_any_kernel(Params p) {
+// through LDS, the next one on its way into registers meanwhile.
+template <typename T, typename TO, ActCode A, bool ODD>
+__global__ __launch_bounds__(256) void staged_kernel(Params p) {
     __shared__ uint4 tile[2][64 * 8];   // x and w: 64 rows of 8 chunks of 8 elements
     const int tm = fdiv(blockIdx.x, p.d_tiles_n), tn = blockIdx.x - tm * p.tiles_n;
     const int m0 = tm * 64, n0 = tn * 64;
@@ -93,8 +169,8 @@ __global__ __launch_bounds__(256) void matmul_any_kernel(Params p) {
     auto fetch = [&](int k) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            xs[i] = load8(xr[i], k + 8 * q, p.K, xok[i]);
-            ws[i] = load8(wr[i], k + 8 * q, p.K, wok[i]);
+            xs[i] = load_cut<ODD>(xr[i], k + 8 * q, xok[i] ? p.K : 0);
+            ws[i] = load_cut<ODD>(wr[i], k + 8 * q, wok[i] ? p.K : 0);
         }
     };
     f32x4 acc[2][2] = {};
@@ -126,42 +202,580 @@ __global__ __launch_bounds__(256) void matmul_any_kernel(Params p) {
     }
     // w is the left operand: a lane holds four consecutive columns of one row of y
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+        const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
+        float bias[4];
+        load_bias(p, n, bias);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int m = m0 + wm + 16 * i + (lane & 15), n = n0 + wn + 16 * j + 4 * (lane >> 4);
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + wm + 16 * i + (lane & 15);
             float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (m < p.M && n < p.N) finish<4, TO, A>(p, m, n, v);
+            if (m < p.M && n < p.N) finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
         }
+    }
+}
+
+// ---- tiles staged by transfers to LDS
+
+constexpr unsigned OOB = 0x80000000u;   // byte offset past every row block: the transfer brings zeros
+
+// The tile a workgroup computes.  Every die gets a contiguous run of workgroups; runs go through panels of 8 tile rows column
+// by column, so that the 32 CUs of a die share few rows of x and w in their L2 at any time.
+struct Tile {
+    int m, n, split;
+};
+__device__ __forceinline__ Tile tile_of(const Params &p, int id) {
+    constexpr int PANEL = 8;
+    const int tiles = p.tiles_m * p.tiles_n;
+    Tile t;
+    t.split = fdiv(id, p.d_tiles);
+    id -= t.split * tiles;
+    const int panel = fdiv(id >> 3, p.d_tiles_n), first = panel * PANEL, rows = min(PANEL, p.tiles_m - first);
+    id -= first * p.tiles_n;
+    t.n = id / rows;
+    t.m = first + id - t.n * rows;
+    return t;
+}
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+__device__ __forceinline__ i32x4 make_rsrc(const void *ptr, unsigned bytes) {
+    const unsigned long long a = reinterpret_cast<unsigned long long>(ptr);
+    return i32x4{__builtin_amdgcn_readfirstlane(static_cast<int>(a)), __builtin_amdgcn_readfirstlane(static_cast<int>((a >> 32) & 0xFFFF)),
+                 __builtin_amdgcn_readfirstlane(static_cast<int>(bytes)), 0x00020000};
+}
+__device__ __forceinline__ unsigned lds_addr(const void *p) {
+    return static_cast<unsigned>(reinterpret_cast<unsigned long long>((const __attribute__((address_space(3))) char *)p));
+}
+// Lane i's 16 bytes at byte offset voff + soff of the buffer go to LDS address base + 16 i.  Issued as assembly so that only
+// this kernel's own waits wait for it.  M0 is written undeclared: the compiler keeps nothing in it.
+__device__ __forceinline__ void dma16(const i32x4 rsrc, unsigned base, unsigned voff, int soff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(base), "v"(voff), "s"(rsrc), "s"(soff)
+                 : "memory");
+}
+
+// A tile of BM rows by BN columns of y, the depth in slices of 64 through two LDS buffers: while one is multiplied the next
+// slice is on its way into the other, and other workgroups of the CU have theirs.  WM x WN wavefronts, each with
+// (BM / WM) x (BN / WN) of the tile in 16 x 16 blocks.
+//
+// Rows of a slice are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), so that the 16 rows of a fragment read come
+// from all 64 banks.  The lane that fills a place fetches the chunk that belongs there.
+//
+// w is the left operand: a lane's accumulators are four consecutive rows of the block, which are columns of y.  Row s of
+// block j of a wavefront's columns is stored column (s / 4) * 4 NB + 4 j + s % 4, which makes the NB blocks of a lane 4 NB
+// consecutive columns: stores of 16 bytes and whole lines without a pass through LDS.
+//
+// Measured and left: rings of four buffers (fewer workgroups a CU, 6272 x 1024 x 4096 71 us instead of 56), fragments read
+// one half slice ahead (68), slices of 32 (half the rate of transfers), lines brought into L2 five slices ahead (no change).
+template <typename T, typename TO, ActCode A, int BM, int BN, int WM, int WN, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Params p) {
+    constexpr int WAVES = WM * WN, MB = BM / WM / 16, NB = BN / WN / 16;
+    constexpr int ROWS = BM + BN, PIECES = ROWS / 8 / WAVES;   // transfers of 8 rows a wavefront issues per slice
+    constexpr int XP = BM / 8 / WAVES, NC = 4 * NB;
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole pieces");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][ROWS * 128];
+    const int id = die_block(p.per_die, blockIdx.x);
+    if (id >= p.total) return;
+    const Tile t = tile_of(p, id);
+    const int m0 = t.m * BM, n0 = t.n * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wm = wave / WN, wn = wave % WN;
+    const int mrows = min(BM, p.M - m0), nrows = min(BN, p.N - n0);
+    const i32x4 xs = make_rsrc(static_cast<const T *>(p.x) + static_cast<long long>(m0) * p.ldx, 2u * ((mrows - 1) * p.ldx + p.K));
+    const i32x4 ws = make_rsrc(static_cast<const T *>(p.w) + static_cast<long long>(n0) * p.ldw, 2u * ((nrows - 1) * p.ldw + p.K));
+    const int k0 = SPLIT ? t.split * p.slices * 64 : 0, k1 = SPLIT ? min(p.K, k0 + p.slices * 64) : p.K;
+    const int n_slices = (k1 - k0 + 63) >> 6;
+
+    // piece j of this wavefront: LDS rows 8 (wave + WAVES j) on; x rows first, then w rows
+    unsigned voff[PIECES];
+    const int q = lane & 7;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+        const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
+        const int chunk = q ^ ((row >> 1) & 7);
+        if (j < XP) {
+            voff[j] = row < mrows ? static_cast<unsigned>(row * p.ldx + chunk * 8) * 2u : OOB;
+        } else {
+            const int in = row % (16 * NB), blk = in >> 4, s = in & 15;
+            const int col = row - in + (s >> 2) * NC + blk * 4 + (s & 3);
+            voff[j] = col < nrows ? static_cast<unsigned>(col * p.ldw + chunk * 8) * 2u : OOB;
+        }
+    }
+    const unsigned base = lds_addr(lds);
+    auto fetch = [&](int s) {
+        const int k = k0 + s * 64;
+        const unsigned to = base + (s & 1) * ROWS * 128 + wave * 1024;
+        const bool cut = k + 64 > p.K;   // the last slice may be short: its missing chunks are zeros
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            unsigned v = voff[j];
+            if (cut) {
+                const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
+                if (k + 8 * (q ^ ((row >> 1) & 7)) >= p.K) v = OOB;
+            }
+            dma16(j < XP ? xs : ws, to + (j < XP ? j * WAVES : BM / 8 + (j - XP) * WAVES) * 1024, v, k * 2);
+        }
+    };
+    f32x4 acc[MB][NB] = {};
+    fetch(0);
+    // fragment rows of this lane: the same swizzle for all blocks, since blocks are 16 rows apart
+    const int fr = lane & 15, key = (fr >> 1) & 7;
+    const int xr = (wm * (BM / WM) + fr) * 128, wr = (BM + wn * (BN / WN) + fr) * 128;
+    const int c0 = ((lane >> 4) ^ key) * 16, c1 = ((4 + (lane >> 4)) ^ key) * 16;
+    for (int s = 0; s < n_slices; ++s) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (s + 1 < n_slices) fetch(s + 1);
+        const unsigned char *buf = lds[s & 1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = h ? c1 : c0;
+            uint4 a[NB], b[MB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) a[j] = *reinterpret_cast<const uint4 *>(buf + wr + j * 2048 + c);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) b[i] = *reinterpret_cast<const uint4 *>(buf + xr + i * 2048 + c);
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[j], b[i], acc[i][j], T());
+        }
+    }
+    const int n = n0 + wn * (BN / WN) + (lane >> 4) * NC;
+    float bias[NC];
+    if (!SPLIT) load_bias(p, n, bias);
+    const bool full = p.vec && n + NC <= p.N;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const int m = m0 + wm * (BM / WM) + 16 * i + fr;
+        if (m >= p.M || n >= p.N) continue;
+        float v[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) v[j] = acc[i][j >> 2][j & 3];
+        if constexpr (SPLIT) {
+            float *y = p.part + (static_cast<size_t>(t.split) * p.M + m) * p.N + n;
+            if (n + NC <= p.N && p.N % 4 == 0) {
+#pragma unroll
+                for (int j = 0; j < NC; j += 4) *reinterpret_cast<float4 *>(y + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+                    if (n + j < p.N) y[j] = v[j];
+            }
+        } else {
+            finish<NC, TO, A>(p, m, n, full, bias, v);
+        }
+    }
+}
+
+// A tile of BM x BM (256 x 256: 160 KB of LDS, one workgroup a CU) with layouts as above.  Slots hold one operand's slice; x
+// of slice s is number 2 s, w number 2 s + 1, number i lies in slot i % 5.  Fragments are read half a slice ahead.  A slice is
+// free once the fragments of its second half are in registers; w of slice s + 2 then takes the place of x of slice s, and
+// x of slice s + 3 that of w.
+template <typename T, typename TO, ActCode A, int BM, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
+    constexpr int BN = BM, NBUF = 5;
+    constexpr int WAVES = WM * WN, MB = BM / WM / 16, NB = BN / WN / 16;
+    constexpr int ROWS = BM + BN, PIECES = ROWS / 8 / WAVES;   // transfers of 8 rows a wavefront issues per slice
+    constexpr int XP = BM / 8 / WAVES, NC = 4 * NB;
+    static_assert(BM == BN && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole pieces");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NBUF * BM * 128];
+    const int id = die_block(p.per_die, blockIdx.x);
+    if (id >= p.total) return;
+    const Tile t = tile_of(p, id);
+    const int m0 = t.m * BM, n0 = t.n * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wm = wave / WN, wn = wave % WN;
+    const int mrows = min(BM, p.M - m0), nrows = min(BN, p.N - n0);
+    const i32x4 xs = make_rsrc(static_cast<const T *>(p.x) + static_cast<long long>(m0) * p.ldx, 2u * ((mrows - 1) * p.ldx + p.K));
+    const i32x4 ws = make_rsrc(static_cast<const T *>(p.w) + static_cast<long long>(n0) * p.ldw, 2u * ((nrows - 1) * p.ldw + p.K));
+    const int n_slices = (p.K + 63) >> 6;
+
+    // piece j of this wavefront: LDS rows 8 (wave + WAVES j) on; x rows first, then w rows
+    unsigned voff[PIECES];
+    const int q = lane & 7;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+        const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
+        const int chunk = q ^ ((row >> 1) & 7);
+        if (j < XP) {
+            voff[j] = row < mrows ? static_cast<unsigned>(row * p.ldx + chunk * 8) * 2u : OOB;
+        } else {
+            const int in = row % (16 * NB), blk = in >> 4, s = in & 15;
+            const int col = row - in + (s >> 2) * NC + blk * 4 + (s & 3);
+            voff[j] = col < nrows ? static_cast<unsigned>(col * p.ldw + chunk * 8) * 2u : OOB;
+        }
+    }
+    const unsigned base = lds_addr(lds);
+    auto piece = [&](bool w, int j, int s, int slot) {
+        const int k = s * 64;
+        unsigned v = voff[j + (w ? XP : 0)];
+        if (k + 64 > p.K) {   // the last slice may be short: its missing chunks are zeros
+            const int row = 8 * (wave + WAVES * j) + (lane >> 3);
+            if (k + 8 * (q ^ ((row >> 1) & 7)) >= p.K) v = OOB;
+        }
+        dma16(w ? ws : xs, base + slot * BM * 128 + wave * 1024 + j * WAVES * 1024, v, k * 2);
+    };
+    auto fetch = [&](bool w, int s, int slot) {
+#pragma unroll
+        for (int j = 0; j < XP; ++j) piece(w, j, s, slot);
+    };
+    f32x4 acc[MB][NB] = {};
+    // fragment rows of this lane: the same swizzle for all blocks, since blocks are 16 rows apart
+    const int fr = lane & 15, key = (fr >> 1) & 7;
+    const int xr = (wm * (BM / WM) + fr) * 128, wr = (wn * (BN / WN) + fr) * 128;
+    const int c0 = ((lane >> 4) ^ key) * 16, c1 = ((4 + (lane >> 4)) ^ key) * 16;
+    auto frag = [&](int off) { return *reinterpret_cast<const uint4 *>(lds + off); };
+    auto read = [&](uint4 (&a)[NB], uint4 (&b)[MB], int xslot, int wslot, int c) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) a[j] = frag(wslot * BM * 128 + wr + c + j * 2048);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) b[i] = frag(xslot * BM * 128 + xr + c + i * 2048);
+    };
+    // The products of half a slice; between them the transfers of one operand of a later slice are requested, one at a time:
+    // requested at once they fill the queue to memory and hold up the matrix instructions behind them (8192^3 886 us, one
+    // at a time 824).
+    auto multiply = [&](const uint4 (&a)[NB], const uint4 (&b)[MB], bool fill, bool w, int s, int slot) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            if (fill) {
+#pragma unroll
+                for (int j = i * XP / MB; j < (i + 1) * XP / MB; ++j) piece(w, j, s, slot);
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[j], b[i], acc[i][j], T());
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < NBUF; ++i)
+        if (i / 2 < n_slices) fetch(i & 1, i / 2, i);
+    uint4 a0[NB], b0[MB], a1[NB], b1[MB];
+    if (n_slices >= 3) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(XP * 3) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    read(a0, b0, 0, 1, c0);
+    int at = 0;   // slot of x of slice s; w's is the next one
+    auto wrap = [](int i) { return i >= NBUF ? i - NBUF : i; };
+    for (int s = 0; s < n_slices; ++s) {
+        const int wat = wrap(at + 1);
+        read(a1, b1, at, wat, c1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(a0, b0, s > 0 && s + 2 < n_slices, false, s + 2, wrap(at + NBUF - 1));
+        const int next = wrap(at + 2);
+        if (s + 1 < n_slices) {
+            // every wavefront has read all of slice s, and slice s + 1 is there; x of slice s + 2 may be on its way
+            if (s + 2 < n_slices) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(XP) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            read(a0, b0, next, wrap(next + 1), c0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(a1, b1, s + 2 < n_slices, true, s + 2, at);
+        at = next;
+    }
+    const int n = n0 + wn * (BN / WN) + (lane >> 4) * NC;
+    float bias[NC];
+    load_bias(p, n, bias);
+    const bool full = p.vec && n + NC <= p.N;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const int m = m0 + wm * (BM / WM) + 16 * i + fr;
+        if (m >= p.M || n >= p.N) continue;
+        float v[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) v[j] = acc[i][j >> 2][j & 3];
+        finish<NC, TO, A>(p, m, n, full, bias, v);
+    }
+}
+
+// ---- few rows or few tiles: no LDS in the main loop
+
+// 16 MB rows by 16 NB columns of y a workgroup, its wavefronts each with a range of the depth and operands straight from
+// memory into the matrix instructions; their sums meet in LDS.  Rows may start at any element.  A wavefront has U steps of 32
+// of the depth in flight: what bounds the form is how long memory takes to answer, so everything is asked for at once.
+template <typename T, typename TO, ActCode A, int MB, int NB, int WAVES, bool ODD>
+__global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
+    constexpr int U = 4, ITEMS = MB * NB * 64;
+    __shared__ f32x4 sums[WAVES][ITEMS];
+    const int id = die_block(p.per_die, blockIdx.x);
+    if (id >= p.total) return;
+    const int tn = fdiv(id, p.d_tiles_m), tm = id - tn * p.tiles_m;   // the row blocks of a column block next to one another
+    const int m0 = tm * 16 * MB, n0 = tn * 16 * NB;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int k0 = wave * p.slices * 32, k1 = min(p.K, k0 + p.slices * 32);
+    const T *wr[NB], *xr[MB];   // rows behind the last are read as the last; what comes of them is not stored
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        wr[j] = static_cast<const T *>(p.w) + static_cast<long long>(min(n0 + 16 * j + (lane & 15), p.N - 1)) * p.ldw;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+        xr[i] = static_cast<const T *>(p.x) + static_cast<long long>(min(m0 + 16 * i + (lane & 15), p.M - 1)) * p.ldx;
+    f32x4 acc[MB][NB] = {};
+    int k = k0 + 8 * (lane >> 4);
+    for (; k - 8 * (lane >> 4) + 32 * U <= k1; k += 32 * U) {
+        uint4 a[U][NB], b[U][MB];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) a[u][j] = load_whole<ODD>(wr[j], k + 32 * u);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) b[u][i] = load_whole<ODD>(xr[i], k + 32 * u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[u][j], b[u][i], acc[i][j], T());
+    }
+    if (k - 8 * (lane >> 4) < k1) {   // the rest, its last chunk perhaps short
+        uint4 a[U][NB], b[U][MB];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) a[u][j] = load_cut<ODD>(wr[j], k + 32 * u, k1);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) b[u][i] = load_cut<ODD>(xr[i], k + 32 * u, k1);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[u][j], b[u][i], acc[i][j], T());
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[wave][(i * NB + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int item = threadIdx.x; item < ITEMS; item += 64 * WAVES) {
+        f32x4 s = sums[0][item];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s += sums[i][item];
+        const int blk = item >> 6, l = item & 63;
+        const int m = m0 + 16 * (blk / NB) + (l & 15), n = n0 + 16 * (blk % NB) + 4 * (l >> 4);
+        if (m >= p.M || n >= p.N) continue;
+        float v[4] = {s[0], s[1], s[2], s[3]}, bias[4];
+        load_bias(p, n, bias);
+        finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
+    }
+}
+
+// ---- a depth that several workgroups share
+
+// Adds the partial sums of a tile kernel in the order of their splits.  A thread takes four columns of a row.
+template <typename TO, ActCode A>
+__global__ __launch_bounds__(256) void join_kernel(Params p) {
+    const unsigned i = blockIdx.x * 256u + threadIdx.x, groups = (p.N + 3) / 4;
+    const unsigned m = i / groups;
+    const int n = static_cast<int>(i - m * groups) * 4;
+    if (m >= static_cast<unsigned>(p.M)) return;
+    const size_t plane = static_cast<size_t>(p.M) * p.N, at = static_cast<size_t>(m) * p.N + n;
+    float v[4] = {}, bias[4];
+    load_bias(p, n, bias);
+    if (p.N % 4 == 0) {
+        f32x4 s = *reinterpret_cast<const f32x4 *>(p.part + at);
+#pragma unroll 8
+        for (int k = 1; k < p.splits; ++k) s += *reinterpret_cast<const f32x4 *>(p.part + k * plane + at);
+        v[0] = s[0]; v[1] = s[1]; v[2] = s[2]; v[3] = s[3];
+    } else {
+        for (int k = 0; k < p.splits; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n + j < p.N) v[j] += p.part[k * plane + at + j];
+    }
+    finish<4, TO, A>(p, static_cast<int>(m), n, p.vec && n + 4 <= p.N, bias, v);
+}
+
+// ---- host side
+
+enum Form { DIRECT4, DIRECT8, DIRECT22, TILE64, TILE128x64, TILE128, BIG, STAGED };
+
+// Microseconds of a form as fitted to 90 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192 (the fastest
+// of the forms 4 % faster than the one chosen, geometric mean):
+//   start + (slices a CU goes through, one after the other) * (time of a slice) + (tiles of the busiest CU) * finish
+// where a slice takes `alone` when it has the CU for itself and `busy` times the workgroups that share it.
+struct TileCost {
+    int bm, bn, resident;
+    double start, alone, busy, finish;
+};
+constexpr TileCost kTile64 = {64, 64, 5, 2.4, 0.32, 0.24, 0.46}, kTile128x64 = {128, 64, 3, 2.2, 0.46, 0.35, 1.0},
+                   kTile128 = {128, 128, 2, 1.2, 0.62, 0.48, 3.2}, kBig = {256, 256, 1, 1.0, 1.27, 1.27, 5.7},
+                   kStaged = {64, 64, 5, 2.5, 0.70, 0.26, 0.46};
+// A direct form takes what its operands take at `per_kb` or its batches of loads one after the other, whichever is longer.
+struct DirectCost {
+    int mb, nb, waves, resident;
+    double start, batch, per_kb;
+};
+constexpr DirectCost kDirect4 = {1, 1, 4, 8, 2.4, 0.48, 0.022}, kDirect8 = {1, 1, 8, 4, 2.4, 0.62, 0.023},
+                     kDirect22 = {2, 2, 8, 2, 2.0, 1.47, 0.027};
+// The launch that joins a shared depth: itself and what the host needs for it, and its traffic by the megabyte.
+constexpr double kJoin = 4.5, kJoinMb = 0.35;
+constexpr int kMaxSplit = 8;
+
+int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+double tile_cost(const TileCost &c, const MatmulArgs &a, int split, int n_cu) {
+    const double tiles = 1.0 * ceil_div(a.M, c.bm) * ceil_div(a.N, c.bn) * split;
+    const int n = static_cast<int>((tiles + n_cu - 1) / n_cu), slices = ceil_div(ceil_div(a.K, 64), split);
+    auto slice = [&](int wgs) { return std::max(c.alone, c.busy * wgs); };
+    const int rest = n % c.resident;
+    double t = c.start + slices * (n / c.resident * slice(c.resident) + (rest ? slice(rest) : 0.0)) + c.finish * n;
+    if (split > 1) t += kJoin + kJoinMb * 4e-6 * split * a.M * a.N;
+    return t;
+}
+
+double direct_cost(const DirectCost &c, const MatmulArgs &a, int n_cu, double slower) {
+    const double wgs = 1.0 * ceil_div(a.M, 16 * c.mb) * ceil_div(a.N, 16 * c.nb);
+    if (wgs > (1 << 20)) return 1e30;   // grids stay below 2^32 threads
+    const int n = static_cast<int>((wgs + n_cu - 1) / n_cu);
+    const double kb = (std::min(a.M, 16 * c.mb) + std::min(a.N, 16 * c.nb)) * (a.K * 2.0 / 1024);
+    return c.start + slower * std::max(1.0 * ceil_div(n, c.resident) * ceil_div(a.K, 128 * c.waves) * c.batch, n * kb * c.per_kb);
+}
+
+struct Choice {
+    Form form;
+    int split;
+};
+
+// rows16: rows of x and w start at multiples of 16 bytes and K is a multiple of 8.  odd: some row may not start at a multiple
+// of 4 bytes.
+Choice choose_form(const MatmulArgs &a, bool rows16, bool odd, int n_cu, size_t ws_bytes) {
+    Choice best{STAGED, 1};
+    double t = 1e30;
+    auto consider = [&](Form f, int split, double cost) {
+        if (cost < t) {
+            t = cost;
+            best = Choice{f, split};
+        }
+    };
+    const double slower = odd ? 1.5 : rows16 ? 1.0 : 1.2;
+    consider(DIRECT4, 1, direct_cost(kDirect4, a, n_cu, slower));
+    consider(DIRECT8, 1, direct_cost(kDirect8, a, n_cu, slower));
+    consider(DIRECT22, 1, direct_cost(kDirect22, a, n_cu, slower));
+    if (!rows16) {
+        consider(STAGED, 1, tile_cost(kStaged, a, 1, n_cu));
+        return best;
+    }
+    consider(TILE64, 1, tile_cost(kTile64, a, 1, n_cu));
+    consider(TILE128x64, 1, tile_cost(kTile128x64, a, 1, n_cu));
+    consider(TILE128, 1, tile_cost(kTile128, a, 1, n_cu));
+    consider(BIG, 1, tile_cost(kBig, a, 1, n_cu));
+    const size_t plane = 4ull * a.M * a.N;
+    if (plane >= (1ull << 32)) return best;
+    for (int split = 2; split <= kMaxSplit && split * plane <= ws_bytes && split <= ceil_div(a.K, 64); split *= 2) {
+        consider(TILE64, split, tile_cost(kTile64, a, split, n_cu));
+        consider(TILE128, split, tile_cost(kTile128, a, split, n_cu));
+    }
+    return best;
+}
+
+template <int BM, int BN>
+dim3 set_grid(Params &p) {
+    p.tiles_m = ceil_div(p.M, BM);
+    p.tiles_n = ceil_div(p.N, BN);
+    p.d_tiles = make_fastdiv(p.tiles_m * p.tiles_n);
+    p.d_tiles_n = make_fastdiv(p.tiles_n);
+    p.d_tiles_m = make_fastdiv(p.tiles_m);
+    p.total = p.tiles_m * p.tiles_n * p.splits;
+    p.per_die = (p.total + 7) / 8;
+    return dim3(8 * p.per_die);
+}
+
+template <typename T, typename TO, ActCode A, int MB, int NB, int WAVES>
+void launch_direct(Params &p, bool odd, hipStream_t stream) {
+    const dim3 grid = set_grid<16 * MB, 16 * NB>(p);
+    p.slices = ceil_div(p.K, 32 * WAVES);
+    if (odd) direct_kernel<T, TO, A, MB, NB, WAVES, true><<<grid, 64 * WAVES, 0, stream>>>(p);
+    else direct_kernel<T, TO, A, MB, NB, WAVES, false><<<grid, 64 * WAVES, 0, stream>>>(p);
+}
+
+template <typename T, typename TO, ActCode A, int BM, int BN>
+void launch_tile(Params &p, hipStream_t stream) {
+    const dim3 grid = set_grid<BM, BN>(p);
+    tile_kernel<T, TO, A, BM, BN, 2, 2, false><<<grid, 256, 0, stream>>>(p);
+}
+
+template <typename T, typename TO, ActCode A, int BM, int BN>
+hipError_t launch_split(Params &p, hipStream_t stream) {
+    const int slices = ceil_div(p.K, 64);
+    p.slices = ceil_div(slices, p.splits);
+    p.splits = ceil_div(slices, p.slices);   // none without a slice
+    const dim3 grid = set_grid<BM, BN>(p);
+    tile_kernel<T, float, ActCode::LINEAR, BM, BN, 2, 2, true><<<grid, 256, 0, stream>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const size_t threads = static_cast<size_t>(p.M) * ceil_div(p.N, 4);
+    join_kernel<TO, A><<<dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T, typename TO, ActCode A>
+hipError_t launch_act(Params &p, const Choice &c, bool odd, hipStream_t stream) {
+    if (p.splits > 1)
+        return c.form == TILE64 ? launch_split<T, TO, A, 64, 64>(p, stream) : launch_split<T, TO, A, 128, 128>(p, stream);
+    switch (c.form) {
+        case DIRECT4: launch_direct<T, TO, A, 1, 1, 4>(p, odd, stream); break;
+        case DIRECT8: launch_direct<T, TO, A, 1, 1, 8>(p, odd, stream); break;
+        case DIRECT22: launch_direct<T, TO, A, 2, 2, 8>(p, odd, stream); break;
+        case TILE64: launch_tile<T, TO, A, 64, 64>(p, stream); break;
+        case TILE128x64: launch_tile<T, TO, A, 128, 64>(p, stream); break;
+        case TILE128: launch_tile<T, TO, A, 128, 128>(p, stream); break;
+        case BIG: {
+            const dim3 grid = set_grid<256, 256>(p);
+            big_tile_kernel<T, TO, A, 256, 2, 4><<<grid, 512, 0, stream>>>(p);
+            break;
+        }
+        case STAGED: {
+            set_grid<64, 64>(p);
+            if (odd) staged_kernel<T, TO, A, true><<<dim3(p.total), 256, 0, stream>>>(p);
+            else staged_kernel<T, TO, A, false><<<dim3(p.total), 256, 0, stream>>>(p);
+            break;
+        }
+    }
+    return hipGetLastError();
 }
 
 template <typename T, typename TO>
-hipError_t launch_any(const Params &p, int tiles_m, hipStream_t stream) {
-    const dim3 grid(tiles_m * p.tiles_n);
+hipError_t launch_types(Params &p, const Choice &c, bool odd, hipStream_t stream) {
     switch (act_code(p.act)) {
-        case ActCode::NORMAL: matmul_any_kernel<T, TO, ActCode::NORMAL><<<grid, 256, 0, stream>>>(p); break;
-        case ActCode::GATE: matmul_any_kernel<T, TO, ActCode::GATE><<<grid, 256, 0, stream>>>(p); break;
-        default: matmul_any_kernel<T, TO, ActCode::LINEAR><<<grid, 256, 0, stream>>>(p);
+        case ActCode::NORMAL: return launch_act<T, TO, ActCode::NORMAL>(p, c, odd, stream);
+        case ActCode::GATE: return launch_act<T, TO, ActCode::GATE>(p, c, odd, stream);
+        default: return launch_act<T, TO, ActCode::LINEAR>(p, c, odd, stream);
     }
-    return hipGetLastError();
+}
+
+bool aligned(const void *q, int ld, int n) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % n == 0); }
+bool rows_aligned(const MatmulArgs &a) { return aligned(a.x, a.ldx, 8) && aligned(a.w, a.ldw, 8) && a.K % 8 == 0; }
+bool rows_odd(const MatmulArgs &a) {
+    return (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 4 != 0 || ((a.ldx | a.ldw) & 1) != 0;
 }
 
 }  // namespace
 
 hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream) {
+    const bool odd = rows_odd(a);
+    const Choice c = choose_form(a, rows_aligned(a), odd, ctx.n_cu, a.ws ? a.ws_bytes : 0);
     Params p{};
     p.x = a.x; p.w = a.w; p.b = a.b; p.r = a.residual; p.y = a.y;
     p.M = a.M; p.N = a.N; p.K = a.K;
     p.ldx = a.ldx; p.ldw = a.ldw; p.ldr = a.ldr; p.ldy = a.ldy;
     p.act = a.act;
-    p.tiles_n = (a.N + 63) / 64;
-    p.d_tiles_n = make_fastdiv(p.tiles_n);
-    const int tiles_m = (a.M + 63) / 64;
+    p.splits = c.split;
+    p.part = static_cast<float *>(a.ws);
+    const int per = a.out_dtype == GPULET_F32 ? 4 : 8;
+    p.vec = aligned(a.y, a.ldy, per) && aligned(a.residual, a.ldr, per);
     if (a.dtype == GPULET_BF16)
-        return a.out_dtype == GPULET_F32 ? launch_any<__bf16, float>(p, tiles_m, stream) : launch_any<__bf16, __bf16>(p, tiles_m, stream);
-    return a.out_dtype == GPULET_F32 ? launch_any<_Float16, float>(p, tiles_m, stream) : launch_any<_Float16, _Float16>(p, tiles_m, stream);
+        return a.out_dtype == GPULET_F32 ? launch_types<__bf16, float>(p, c, odd, stream) : launch_types<__bf16, __bf16>(p, c, odd, stream);
+    return a.out_dtype == GPULET_F32 ? launch_types<_Float16, float>(p, c, odd, stream)
+                                     : launch_types<_Float16, _Float16>(p, c, odd, stream);
 }
 
-size_t matmul_workspace(const MatmulArgs &a) { return 0; }
+size_t matmul_workspace(const MatmulArgs &a) {
+    int split = 1;
+    for (int n_cu = 32; n_cu <= 256; n_cu += 32)
+        split = std::max(split, choose_form(a, rows_aligned(a), rows_odd(a), n_cu, ~static_cast<size_t>(0)).split);
+    return split == 1 ? 0 : (4ull * split * a.M * a.N + 255) / 256 * 256;
+}
 
 }  // namespace gpulet
