@@ -567,7 +567,14 @@ gpulet_status gpulet_group_norm(const gpulet_group_norm_desc *d, void *workspace
  * Whole model on a gpu-let (Sec. 5 "Backend inference executor").
  * ------------------------------------------------------------------------ */
 
-enum { GPULET_OP_CONV = 0, GPULET_OP_POOL = 1, GPULET_OP_FC = 2, GPULET_OP_DWCONV = 3 };
+enum {
+    GPULET_OP_CONV = 0,
+    GPULET_OP_POOL = 1,
+    GPULET_OP_FC = 2,
+    GPULET_OP_DWCONV = 3,
+    GPULET_OP_GROUP_NORM = 4, /* gpulet_group_norm on bf16 maps */
+    GPULET_OP_MATMUL = 5      /* gpulet_matmul on the pixels of bf16 maps: every pixel's C channels to K */
+};
 
 /*
  * One layer.  Activations live in numbered buffers; a layer reads in_buf and
@@ -578,19 +585,19 @@ typedef struct gpulet_layer {
     int32_t op;            /* GPULET_OP_* */
     int32_t in_buf;        /* buffer read */
     int32_t out_buf;       /* buffer written */
-    int32_t res_buf;       /* CONV: buffer added before the ReLU, or -1 */
-    int32_t C;             /* CONV/DWCONV/POOL: input channels; FC: In (= C*H*W of in_buf) */
-    int32_t K;             /* CONV: output channels; FC: Out */
+    int32_t res_buf;       /* CONV/GROUP_NORM/MATMUL: buffer added before the activation, or -1 */
+    int32_t C;             /* CONV/DWCONV/POOL/GROUP_NORM/MATMUL: input channels; FC: In (= C*H*W of in_buf) */
+    int32_t K;             /* CONV/MATMUL: output channels; FC: Out; GROUP_NORM: groups */
     int32_t R;             /* CONV/DWCONV: kernel height; POOL: window k */
     int32_t S;             /* CONV/DWCONV: kernel width */
     int32_t stride;
     int32_t pad;
-    int32_t relu;          /* CONV/DWCONV/FC */
+    int32_t relu;          /* CONV/DWCONV/FC; GROUP_NORM/MATMUL: GPULET_ACT_* */
     int32_t mode;          /* POOL: GPULET_POOL_* */
     int32_t out_ch_total;  /* CONV: channels of out_buf when this layer writes a slice of
                               a concatenated tensor; 0 means K */
     int32_t out_ch_offset; /* CONV: first channel written */
-    int32_t out_fp32;      /* FC: store fp32 instead of bf16 */
+    int32_t out_fp32;      /* FC/MATMUL: store fp32 instead of bf16 (MATMUL: res_buf holds fp32 then) */
     int32_t pre_pool;      /* CONV: 0, or 3 = a 3x3 / stride 1 / pad 1 max pool of in_buf comes first
                               (gpulet_maxpool3_conv1x1_fwd; 1x1 filters, stride 1, pad 0, C % 8 == 0) */
     int32_t in_ch_total;   /* CONV: channels of in_buf when this layer reads only C of them (the
@@ -608,8 +615,10 @@ typedef struct gpulet_layer {
     int32_t pool_buf;      /* CONV with side_pool: buffer that receives the pooled tensor */
     int32_t group_next;    /* CONV: 1 = the next layer (a CONV too) is independent of this one and may
                               share its launch (gpulet_conv2d_group_fwd); chains of up to 4 layers */
-    const void *w;         /* device: CONV KRSC bf16, DWCONV RSC bf16, FC [Out][In] bf16 */
-    const float *b;        /* device: fp32 bias or NULL */
+    float eps;             /* GROUP_NORM */
+    const void *w;         /* device: CONV KRSC bf16, DWCONV RSC bf16, FC [Out][In] bf16, MATMUL [K][C] bf16,
+                              GROUP_NORM C fp32 (gamma) or NULL */
+    const float *b;        /* device: fp32 bias or NULL; GROUP_NORM: beta or NULL */
 } gpulet_layer;
 
 /*
@@ -652,7 +661,8 @@ gpulet_status gpulet_model_schedule(const gpulet_model_desc *m, int batch, int l
                                     int *wait_from, int *wait_to, int max_waits, int *n_waits);
 
 /* Bytes of workspace gpulet_run_model needs for `batch` images (a multiple of
- * 256).  GPULET_EINVAL if the description is inconsistent (channel or feature
+ * 256): the buffers, and behind them what GROUP_NORM and MATMUL layers use while
+ * they run.  GPULET_EINVAL if the description is inconsistent (channel or feature
  * counts that do not match the inferred shapes, bad buffer indices, a buffer
  * read before written, empty outputs). */
 gpulet_status gpulet_model_workspace_bytes(const gpulet_model_desc *m, int batch, size_t *bytes);
@@ -671,7 +681,9 @@ gpulet_status gpulet_model_buffer_info(const gpulet_model_desc *m, int batch, in
  * gpulet_model_workspace_bytes() bytes (GPULET_ENOMEM otherwise).
  * Where `in`, `out` and `workspace` overlap, every layer is a launch of its own
  * (a launch that stands for several layers would store to the output while it
- * still reads the input), and no layer may read what it writes itself.
+ * still reads the input), and no layer may read what it writes itself; `in` and
+ * `out` may not overlap the part of the workspace behind the buffers
+ * (GPULET_EINVAL).
  * If latency_ms is not NULL the call brackets the batch with events, waits
  * for it and stores the elapsed milliseconds; if NULL it returns right after
  * enqueueing.  Counts one batch and `batch` images on the partition.

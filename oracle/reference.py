@@ -8,6 +8,7 @@ with no rounding in between; the flatten before the first FC is PyTorch's
 """
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -148,6 +149,42 @@ def depthwise_conv2d(x, w, b=None, stride=1, pad=0, relu=False):
     return y
 
 
+def activation(v, act):
+    """Elementwise activations by name (PyTorch's definitions)."""
+    if act == "none":
+        return v
+    if act == "relu":
+        return np.maximum(v, 0.0)
+    if act == "silu":
+        return v / (1.0 + np.exp(-v))
+    if act == "gelu":
+        return 0.5 * v * (1.0 + np.vectorize(math.erf, otypes=[float])(v / math.sqrt(2.0)))
+    if act == "gelu_tanh":
+        return 0.5 * v * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3)))
+    raise ValueError("unknown activation %r" % (act,))
+
+
+def group_norm(x, gamma, beta, groups, eps, act="none", residual=None):
+    """Group norm of (N,C,H,W): mean and (biased) variance over each group of
+    channels and the plane, then scale, shift, residual and activation."""
+    x = _f64(x)
+    N, C, H, W = x.shape
+    if C % groups:
+        raise ValueError("%d channels in %d groups" % (C, groups))
+    g = x.reshape(N, groups, -1)
+    g = (g - g.mean(axis=2, keepdims=True)) / np.sqrt(g.var(axis=2, keepdims=True) + eps)
+    y = g.reshape(x.shape) * _f64(gamma)[:, None, None] + _f64(beta)[:, None, None]
+    return activation(y if residual is None else y + _f64(residual), act)
+
+
+def pixel_matmul(x, w, b=None, act="none", residual=None):
+    """Product of every pixel's channels of (N,C,H,W) with w (K,C), then bias, residual and activation."""
+    y = np.tensordot(_f64(w), _f64(x), axes=(1, 1)).transpose(1, 0, 2, 3)
+    if b is not None:
+        y = y + _f64(b)[:, None, None]
+    return activation(y if residual is None else y + _f64(residual), act)
+
+
 def run_model(model, params, x, keep=False, storage=None):
     """Forward pass of a ``workloads.Model`` on batch ``x`` (N,C,H,W) in fp64.
 
@@ -176,6 +213,12 @@ def run_model(model, params, x, keep=False, storage=None):
             w, b = params[nd.name]
             src = t[nd.src]
             t[nd.dst] = keep_as(fc(src.reshape(src.shape[0], -1), w, b, a["relu"]))
+        elif nd.op in ("groupnorm", "matmul"):
+            w, b = params[nd.name]
+            src = t[nd.src].reshape(t[nd.src].shape + (1,) * (4 - t[nd.src].ndim))
+            res = t[a["residual"]] if a["residual"] else None
+            t[nd.dst] = keep_as(group_norm(src, w, b, a["groups"], a["eps"], a["act"], res) if nd.op == "groupnorm" else
+                                pixel_matmul(src, w, b, a["act"], res))
         elif nd.op == "concat":
             t[nd.dst] = np.concatenate([t[s] for s in nd.src], axis=1)
         else:
@@ -216,6 +259,14 @@ def model_flops(model):
             assert C * H * W == a["In"], (nd.name, C * H * W, a["In"])
             fcf += 2 * a["In"] * a["Out"]
             shapes[nd.dst] = (a["Out"], 1, 1)
+        elif nd.op == "groupnorm":
+            assert shapes[nd.src][0] == a["C"], nd.name
+            shapes[nd.dst] = shapes[nd.src]
+        elif nd.op == "matmul":
+            C, H, W = shapes[nd.src]
+            assert C == a["C"], (nd.name, C, a["C"])
+            fcf += 2 * H * W * C * a["K"]
+            shapes[nd.dst] = (a["K"], H, W)
         elif nd.op == "concat":
             parts = [shapes[s] for s in nd.src]
             assert all(p[1:] == parts[0][1:] for p in parts), nd.name
@@ -235,6 +286,10 @@ def model_params(model):
             n += a["C"] * a["k"] * a["k"] + a["C"]
         elif nd.op == "fc":
             n += nd.attr["Out"] * nd.attr["In"] + nd.attr["Out"]
+        elif nd.op == "matmul":
+            n += nd.attr["K"] * nd.attr["C"] + nd.attr["K"]
+        elif nd.op == "groupnorm":
+            n += 2 * nd.attr["C"]
     return n
 
 

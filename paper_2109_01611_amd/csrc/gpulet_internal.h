@@ -149,7 +149,8 @@ struct MatmulArgs {
 };
 gpulet_status check_matmul(const gpulet_matmul_desc *d, MatmulArgs &a);
 size_t matmul_workspace(const MatmulArgs &a);   // most bytes launch_matmul can use, whatever the CU count
-hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream);
+// *launches (if not null), here and below: the kernel launches made.
+hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream, int *launches = nullptr);
 struct GroupNormArgs {
     const void *x;
     const float *gamma, *beta;
@@ -162,7 +163,7 @@ struct GroupNormArgs {
 };
 gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a);
 size_t group_norm_workspace(const GroupNormArgs &a);   // bytes launch_group_norm needs
-hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream);
+hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream, int *launches = nullptr);
 
 // image_chain.hip: consecutive small layers, each reading what the one before wrote, as one launch with one
 // workgroup per image.  Every layer takes (C, H, W) to (K, P, Q) per image: convolutions with dense input and

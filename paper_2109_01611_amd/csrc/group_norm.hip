@@ -640,8 +640,9 @@ hipError_t launch_act(const Plan &pl, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream) {
+hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream, int *launches) {
     Plan pl = make_plan(a);
+    if (launches) *launches = pl.form == Plan::TWO ? 2 : 1;
     pl.p.part = pl.q.part = static_cast<float2 *>(a.ws);
     if (a.dtype == GPULET_BF16) return launch_act<__bf16>(pl, stream);
     if (a.dtype == GPULET_F16) return launch_act<_Float16>(pl, stream);

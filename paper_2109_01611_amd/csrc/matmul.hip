@@ -753,9 +753,10 @@ bool rows_odd(const MatmulArgs &a) {
 
 }  // namespace
 
-hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream) {
+hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
     const bool odd = rows_odd(a);
     const Choice c = choose_form(a, rows_aligned(a), odd, ctx.n_cu, a.ws ? a.ws_bytes : 0);
+    if (launches) *launches = c.split > 1 ? 2 : 1;
     Params p{};
     p.x = a.x; p.w = a.w; p.b = a.b; p.r = a.residual; p.y = a.y;
     p.M = a.M; p.N = a.N; p.K = a.K;

@@ -15,6 +15,8 @@
 
 using namespace gpulet;
 
+static_assert(sizeof(gpulet_layer) == 120, "eps lies where the structure had 4 bytes of padding");
+
 namespace {
 
 constexpr size_t kAlign = 256;
@@ -35,6 +37,8 @@ struct Step {
     int In, Out, relu, out_fp32;                     // FC
     const void *w;
     const float *b;
+    gpulet_group_norm_desc norm;                     // GROUP_NORM, tensors filled in at run time
+    gpulet_matmul_desc mm;                           // MATMUL, likewise
     bool slice;             // CONV writing a channel slice of a wider (concatenated) tensor
     bool slice2;            // the same for the second buffer
     int group_len;          // CONV: layers launched together starting here (1: alone; 0: inside a group)
@@ -54,8 +58,13 @@ struct Plan {
     std::vector<BufState> bufs;
     std::vector<size_t> offset;  // workspace offset per buffer, (size_t)-1 for caller-owned
     size_t ws_bytes = 0;
+    size_t op_offset = 0, op_bytes = 0;  // the end of the workspace: scratch of whichever layer runs
     int in_buf = 0, out_buf = 0;
 };
+
+// Addresses that stand for the tensors of a layer while its description is checked: far from one another and from any
+// weights, aligned to `align` bytes and not more.
+void *stand_in(int which, uintptr_t align) { return reinterpret_cast<void *>((static_cast<uintptr_t>(which) << 56) + align); }
 
 // One lane: see gpulet_set_model_lanes.
 std::atomic<int> g_model_lanes{1};
@@ -313,6 +322,37 @@ gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
             if (st != GPULET_OK) return st;
             s.N = batch; s.In = L.C; s.Out = L.K; s.relu = L.relu ? 1 : 0; s.out_fp32 = L.out_fp32 ? 1 : 0;
             oc = L.K; oh = 1; ow = 1; oelem = L.out_fp32 ? 4 : 2;
+        } else if (L.op == GPULET_OP_GROUP_NORM || L.op == GPULET_OP_MATMUL) {
+            if (L.C != src.C) return GPULET_EINVAL;
+            const bool norm = L.op == GPULET_OP_GROUP_NORM;
+            oc = norm ? src.C : L.K; oh = src.H; ow = src.W; oelem = !norm && L.out_fp32 ? 4 : 2;
+            if (L.res_buf >= 0) {
+                if (L.res_buf >= m->n_bufs) return GPULET_EINVAL;
+                const BufState &r = plan.bufs[static_cast<size_t>(L.res_buf)];
+                if (!r.written || r.elem != oelem || r.C != oc || r.H != oh || r.W != ow) return GPULET_EINVAL;
+                s.res_buf = L.res_buf;
+            }
+            void *res = L.res_buf >= 0 ? stand_in(3, 256) : nullptr;
+            if (norm) {
+                s.norm = gpulet_group_norm_desc{stand_in(1, 256), static_cast<const float *>(L.w), L.b, res, stand_in(2, 256), batch,
+                                                src.C, src.H, src.W, L.K, 0, 0, 0, L.eps, GPULET_BF16, L.relu};
+                // the caller's tensors may be aligned less than the buffers, and the scratch depends on that
+                for (uintptr_t align : {256, 8, 4, 2}) {
+                    GroupNormArgs a;
+                    const gpulet_status st = check_group_norm(&s.norm, a);
+                    if (st != GPULET_OK) return st;
+                    if (align != 256) a.x = stand_in(1, align);
+                    plan.op_bytes = std::max(plan.op_bytes, group_norm_workspace(a));
+                }
+            } else {
+                if (1LL * batch * src.H * src.W > INT_MAX) return GPULET_EINVAL;
+                s.mm = gpulet_matmul_desc{stand_in(1, 256), L.w, L.b, res, stand_in(2, 256), batch * src.H * src.W, L.K, src.C,
+                                          0, 0, 0, 0, GPULET_BF16, L.out_fp32 ? GPULET_F32 : GPULET_BF16, L.relu};
+                MatmulArgs a;
+                const gpulet_status st = check_matmul(&s.mm, a);
+                if (st != GPULET_OK) return st;
+                plan.op_bytes = std::max(plan.op_bytes, matmul_workspace(a));
+            }
         } else {
             return GPULET_EINVAL;
         }
@@ -412,7 +452,8 @@ gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
         plan.offset[static_cast<size_t>(i)] = off;
         off += round_up(plan.bufs[static_cast<size_t>(i)].bytes_per_image * static_cast<size_t>(batch));
     }
-    plan.ws_bytes = off;
+    plan.op_offset = off;
+    plan.ws_bytes = off + round_up(plan.op_bytes);
     return GPULET_OK;
 }
 
@@ -470,6 +511,29 @@ bool chain_aligned(const ChainLayer *l, size_t n, const void *x) {
     for (size_t k = 0; k < n; ++k)
         if (l[k].kind != GPULET_OP_FC && reinterpret_cast<uintptr_t>(l[k].y) % 16 != 0) return false;
     return true;
+}
+
+// A GROUP_NORM or MATMUL layer.
+hipError_t run_block_layer(const Bound &bd, const Step &s, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
+    const void *x = bd.ptr(s.in_buf), *res = s.res_buf >= 0 ? bd.ptr(s.res_buf) : nullptr;
+    void *y = bd.ptr(s.out_buf), *scratch = bd.plan->op_bytes > 0 ? bd.ws + bd.plan->op_offset : nullptr;
+    if (s.op == GPULET_OP_GROUP_NORM) {
+        gpulet_group_norm_desc d = s.norm;
+        d.x = x; d.residual = res; d.y = y;
+        GroupNormArgs a;
+        if (check_group_norm(&d, a) != GPULET_OK) return hipErrorInvalidValue;
+        a.ws = scratch;
+        a.ws_bytes = bd.plan->op_bytes;
+        if (group_norm_workspace(a) > a.ws_bytes) return hipErrorInvalidValue;
+        return launch_group_norm(a, stream, launches);
+    }
+    gpulet_matmul_desc d = s.mm;
+    d.x = x; d.residual = res; d.y = y;
+    MatmulArgs a;
+    if (check_matmul(&d, a) != GPULET_OK) return hipErrorInvalidValue;
+    a.ws = scratch;
+    a.ws_bytes = bd.plan->op_bytes;
+    return launch_matmul(a, ctx, stream, launches);
 }
 
 // Enqueues every layer of one batch on the gpu-let's lanes; no host synchronisation.  Lane 0
@@ -625,6 +689,12 @@ hipError_t enqueue(const Bound &bd, gpulet_partition *p) {
         } else if (s.op == GPULET_OP_DWCONV) {
             e = launch_dwconv(bd.ptr(s.in_buf), s.w, s.b, bd.ptr(s.out_buf), s.N, s.C, s.H, s.W, s.k, s.k2,
                               s.stride, s.pad, s.relu, s.P, s.Q, stream);
+        } else if (s.op == GPULET_OP_GROUP_NORM || s.op == GPULET_OP_MATMUL) {
+            // One scratch for all layers: they follow one another on one lane.
+            int launches = 0;
+            e = run_block_layer(bd, s, ctx, stream, &launches);
+            if (e != hipSuccess) return e;
+            p->kernels_enqueued.fetch_add(static_cast<uint64_t>(launches - 1));
         } else {
             e = launch_fc(bd.ptr(s.in_buf), s.w, s.b, bd.ptr(s.out_buf), s.N, s.In, s.Out, s.relu, s.out_fp32, ctx,
                           stream);
@@ -649,12 +719,20 @@ hipError_t enqueue(const Bound &bd, gpulet_partition *p) {
     return hipSuccess;
 }
 
-gpulet_status check_run_args(const Plan &plan, const void *in, void *out, void *ws, size_t ws_bytes) {
+gpulet_status check_run_args(const Plan &plan, int batch, const void *in, void *out, void *ws, size_t ws_bytes) {
     if (!in || !out) return GPULET_EINVAL;
     if (plan.ws_bytes > 0) {
         if (!ws) return GPULET_EINVAL;
         if (ws_bytes < plan.ws_bytes) return GPULET_ENOMEM;
         if (reinterpret_cast<uintptr_t>(ws) % kAlign != 0) return GPULET_EINVAL;
+    }
+    if (plan.op_bytes > 0) {
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(ws) + plan.op_offset, hi = lo + plan.op_bytes;
+        auto meets = [&](const void *p, int buf) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            return at < hi && lo < at + plan.bufs[static_cast<size_t>(buf)].bytes_per_image * static_cast<size_t>(batch);
+        };
+        if (meets(in, plan.in_buf) || meets(out, plan.out_buf)) return GPULET_EINVAL;
     }
     return GPULET_OK;
 }
@@ -760,7 +838,7 @@ extern "C" gpulet_status gpulet_run_model(const gpulet_model_desc *m, int batch,
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, in, out, workspace, workspace_bytes);
+    st = check_run_args(plan, batch, in, out, workspace, workspace_bytes);
     if (st != GPULET_OK) return st;
     const Bound bd{&plan, batch, in, out, static_cast<char *>(workspace)};
     if (latency_ms) {
@@ -785,7 +863,7 @@ extern "C" gpulet_status gpulet_profile_model(const gpulet_model_desc *m, int ba
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, in, out, workspace, workspace_bytes);
+    st = check_run_args(plan, batch, in, out, workspace, workspace_bytes);
     if (st != GPULET_OK) return st;
     const Bound bd{&plan, batch, in, out, static_cast<char *>(workspace)};
 
@@ -874,7 +952,7 @@ extern "C" gpulet_status gpulet_model_graph_create(const gpulet_model_desc *m, i
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, in, out_buf, workspace, workspace_bytes);
+    st = check_run_args(plan, batch, in, out_buf, workspace, workspace_bytes);
     if (st != GPULET_OK) return st;
     const Bound bd{&plan, batch, in, out_buf, static_cast<char *>(workspace)};
     GPULET_HIP(hipStreamSynchronize(p->stream));
@@ -1012,9 +1090,9 @@ extern "C" gpulet_status gpulet_profile_corun(
     if (st != GPULET_OK) return st;
     st = build_plan(mb, batch_b, plan_b);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan_a, in_a, out_a, ws_a, ws_a_bytes);
+    st = check_run_args(plan_a, batch_a, in_a, out_a, ws_a, ws_a_bytes);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan_b, in_b, out_b, ws_b, ws_b_bytes);
+    st = check_run_args(plan_b, batch_b, in_b, out_b, ws_b, ws_b_bytes);
     if (st != GPULET_OK) return st;
 
     CorunSide sa{&plan_a, Bound{&plan_a, batch_a, in_a, out_a, static_cast<char *>(ws_a)}, pa, batch_a, warmup, cap_a, lat_a};

@@ -23,7 +23,7 @@ LIB_PATH = os.path.join(_HERE, "libgpulet.so")
 
 OK, EINVAL, EOVERSUB, EHIP, ENOMEM = 0, -1, -2, -3, -4
 POOL_MAX, POOL_AVG, POOL_GLOBAL_AVG = 0, 1, 2
-OP_CONV, OP_POOL, OP_FC, OP_DWCONV = 0, 1, 2, 3
+OP_CONV, OP_POOL, OP_FC, OP_DWCONV, OP_GROUP_NORM, OP_MATMUL = 0, 1, 2, 3, 4, 5
 BF16, F16, F32 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 CONV_TILES = 15  # GPULET_CONV_TILES: set_conv_tile takes -1 .. CONV_TILES - 1
@@ -44,7 +44,7 @@ class Layer(ctypes.Structure):
         "op", "in_buf", "out_buf", "res_buf", "C", "K", "R", "S", "stride", "pad", "relu", "mode",
         "out_ch_total", "out_ch_offset", "out_fp32", "pre_pool", "in_ch_total", "in_ch_offset", "K2", "out2_buf",
         "out2_ch_total", "out2_ch_offset", "side_pool", "pool_buf",
-        "group_next")] + [("w", c_void_p), ("b", c_void_p)]
+        "group_next")] + [("eps", c_float), ("w", c_void_p), ("b", c_void_p)]
 
 
 class ConvDesc(ctypes.Structure):

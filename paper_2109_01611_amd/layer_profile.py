@@ -72,6 +72,8 @@ def conv_shapes(model, batch):
             shape[nd.dst] = (shape[nd.src][0], 1, 1)
         elif nd.op == "fc":
             shape[nd.dst] = (a["Out"], 1, 1)
+        elif nd.op in ("groupnorm", "matmul"):
+            shape[nd.dst] = (a.get("K", a["C"]),) + shape[nd.src][1:]
         elif nd.op == "concat":
             parts = [shape[s] for s in nd.src]
             shape[nd.dst] = (sum(p[0] for p in parts),) + parts[0][1:]

@@ -54,6 +54,18 @@ def kcrs_to_krsc(w, device):
     return to_device_bf16(np.transpose(w, (0, 2, 3, 1)), device)
 
 
+ACTS = {"none": gpulet.ACT_NONE, "relu": gpulet.ACT_RELU, "silu": gpulet.ACT_SILU, "gelu": gpulet.ACT_GELU,
+        "gelu_tanh": gpulet.ACT_GELU_TANH}
+
+
+def _reads(nd):
+    """The tensors a node reads."""
+    reads = list(nd.src) if nd.op == "concat" else [nd.src]
+    if nd.attr.get("residual"):
+        reads.append(nd.attr["residual"])
+    return reads
+
+
 def _may_share_launch(dw, pw):
     """Whether the library runs a depthwise layer and the 1x1 layer behind it as one launch at some batch and CU count
     (``dwpw_applicable`` in conv_dwpw.hip).  Such a launch stores the pair's output while it still reads the pair's
@@ -95,9 +107,9 @@ class DeviceModel:
         chans = {"x": model.in_shape[0]}
         alias = {}  # concat source -> (concat tensor, channel offset, total channels)
         for nd in nodes:
-            if nd.op == "conv":
+            if nd.op in ("conv", "matmul"):
                 chans[nd.dst] = nd.attr["K"]
-            elif nd.op in ("maxpool", "gavgpool", "dwconv"):
+            elif nd.op in ("maxpool", "gavgpool", "dwconv", "groupnorm"):
                 chans[nd.dst] = chans[nd.src]
             elif nd.op == "fc":
                 chans[nd.dst] = nd.attr["Out"]
@@ -117,9 +129,7 @@ class DeviceModel:
         c_extra = {}         # tensor -> zero channels it carries
         all_readers = {}
         for nd in nodes:
-            reads = list(nd.src) if nd.op == "concat" else [nd.src]
-            if nd.op == "conv" and nd.attr["residual"]:
-                reads.append(nd.attr["residual"])
+            reads = _reads(nd)
             for t in reads:
                 all_readers.setdefault(t, []).append(nd)
         for nd in nodes:
@@ -153,9 +163,7 @@ class DeviceModel:
         if fuse_pools:
             readers = {}
             for nd in nodes:
-                reads = list(nd.src) if nd.op == "concat" else [nd.src]
-                if nd.op == "conv" and nd.attr["residual"]:
-                    reads.append(nd.attr["residual"])
+                reads = _reads(nd)
                 for t in reads:
                     readers.setdefault(t, []).append(nd)
             moved, kept = {}, []
@@ -190,9 +198,7 @@ class DeviceModel:
         # last node index at which each storage tensor is read
         last_use = {}
         for i, nd in enumerate(nodes):
-            reads = list(nd.src) if nd.op == "concat" else [nd.src]
-            if nd.op == "conv" and nd.attr["residual"]:
-                reads.append(nd.attr["residual"])
+            reads = _reads(nd)
             for t in reads:
                 last_use[storage(t)] = i
             # A 2x2 / stride 2 max pool right behind a convolution may be computed by that convolution's
@@ -299,6 +305,23 @@ class DeviceModel:
                 L.op, L.C, L.K, L.relu = gpulet.OP_FC, a["In"], a["Out"], int(a["relu"])
                 L.out_fp32 = int(nd.dst == model.out)
                 L.w, L.b = wd.data_ptr(), bd.data_ptr()
+            elif nd.op in ("groupnorm", "matmul"):
+                w, b = params[nd.name]
+                wd = (to_device_bf16(w, self.device) if nd.op == "matmul" else
+                      torch.from_numpy(np.ascontiguousarray(w, dtype=np.float32)).to(self.device))
+                bd = torch.from_numpy(np.ascontiguousarray(b, dtype=np.float32)).to(self.device)
+                self._keep += [wd, bd]
+                L.C, L.relu = a["C"], ACTS[a["act"]]
+                if nd.op == "matmul":
+                    L.op, L.K = gpulet.OP_MATMUL, a["K"]
+                    L.out_fp32 = int(nd.dst == model.out and not a["residual"])
+                else:
+                    L.op, L.K, L.eps = gpulet.OP_GROUP_NORM, a["groups"], a["eps"]
+                if a["residual"]:
+                    if storage(a["residual"]) != a["residual"]:
+                        raise ValueError("reading a concat slice on its own is not supported")
+                    L.res_buf = buf_of[a["residual"]]
+                L.w, L.b = wd.data_ptr(), bd.data_ptr()
             else:
                 raise ValueError("unknown node kind %r" % (nd.op,))
             layers.append(L)
@@ -319,7 +342,7 @@ class DeviceModel:
         d.in_buf, d.out_buf = 0, 1
         d.layers = self.layers
         self.desc = d
-        self.out_fp32 = producers[model.out].op == "fc"
+        self.out_fp32 = any(L.out_fp32 for L in layers if L.out_buf == 1)
         self._ws = {}
 
     def _stack_siblings(self, nodes, chans, alias, model):
@@ -338,9 +361,7 @@ class DeviceModel:
         """
         readers = {}
         for nd in nodes:
-            reads = list(nd.src) if nd.op == "concat" else [nd.src]
-            if nd.op == "conv" and nd.attr["residual"]:
-                reads.append(nd.attr["residual"])
+            reads = _reads(nd)
             for t in reads:
                 readers.setdefault(t, []).append(nd)
         index = {nd.name: i for i, nd in enumerate(nodes)}
@@ -435,7 +456,7 @@ class DeviceModel:
                     and not a.get("pre_pool") and "in_slice" not in a and nd.src != "x"
                     and nd.src not in alias and chans[nd.src] % 8 == 0):
                 hosts.setdefault(nd.src, (i, nd.name))
-            for t in (list(nd.src) if nd.op == "concat" else [nd.src]):
+            for t in _reads(nd):
                 first_read.setdefault(t, i)
         riders, kept = {}, []
         for i, nd in enumerate(nodes):
@@ -456,19 +477,13 @@ class DeviceModel:
         # tensor is first moved next to its sibling when nothing in between stands in the way (a
         # projection shortcut next to the first layer of its residual block), then runs of
         # adjacent convolutions that neither read nor overwrite one another's tensors are chained.
-        def reads_of(nd):
-            r = list(nd.src) if nd.op == "concat" else [nd.src]
-            if nd.op == "conv" and nd.attr["residual"]:
-                r.append(nd.attr["residual"])
-            return r
-
         def shareable(nd):
             a = nd.attr
             return (nd.op == "conv" and a["C"] % 8 == 0 and nd.src != "x" and not a.get("pre_pool")
                     and "dst2" not in a and "pool_dst" not in a)
 
         def independent(p, q):
-            if p.dst in reads_of(q) or q.dst in reads_of(p):
+            if p.dst in _reads(q) or q.dst in _reads(p):
                 return False
             sp, sq = storage(p.dst), storage(q.dst)
             return sp != sq or (p.dst in alias and q.dst in alias)

@@ -30,7 +30,7 @@ def _extent(n, k, stride, pad):
 
 
 def model_flops(model):
-    """2 * multiply-adds of one image (padding taps counted) as (conv, fc)."""
+    """2 * multiply-adds of one image (padding taps counted) as (conv, fc), per-pixel products counted with fc."""
     shape = {"x": tuple(model.in_shape)}
     conv = fc = 0
     for nd in model.nodes:
@@ -53,6 +53,12 @@ def model_flops(model):
         elif nd.op == "fc":
             fc += 2 * a["In"] * a["Out"]
             shape[nd.dst] = (a["Out"], 1, 1)
+        elif nd.op == "groupnorm":
+            shape[nd.dst] = shape[nd.src]
+        elif nd.op == "matmul":
+            C, H, W = shape[nd.src]
+            fc += 2 * H * W * C * a["K"]
+            shape[nd.dst] = (a["K"], H, W)
         elif nd.op == "concat":
             parts = [shape[s] for s in nd.src]
             shape[nd.dst] = (sum(p[0] for p in parts),) + parts[0][1:]

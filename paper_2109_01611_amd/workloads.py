@@ -18,7 +18,13 @@ Node kinds (all convolutions and pools are square):
   maxpool  src -> dst   k, stride, pad (padding never wins the max)
   gavgpool src -> dst   mean over the whole H x W plane
   fc       src -> dst   In, Out, relu; In is flattened from (C, H, W)
+  groupnorm src -> dst  C, groups, eps, act, optional residual tensor that is
+                        added before the activation
+  matmul   src -> dst   C, K, act, optional residual: every pixel's C channels
+                        to K
   concat   srcs -> dst  along channels
+
+``act`` is one of none, relu, silu, gelu, gelu_tanh.
 """
 
 from collections import namedtuple
@@ -48,6 +54,14 @@ def _gavg(name, src, dst):
 
 def _fc(name, src, dst, In, Out, relu):
     return Node("fc", name, src, dst, dict(In=In, Out=Out, relu=relu))
+
+
+def _groupnorm(name, src, dst, C, groups, act="none", residual=None, eps=1e-5):
+    return Node("groupnorm", name, src, dst, dict(C=C, groups=groups, eps=eps, act=act, residual=residual))
+
+
+def _matmul(name, src, dst, C, K, act="none", residual=None):
+    return Node("matmul", name, src, dst, dict(C=C, K=K, act=act, residual=residual))
 
 
 def _concat(name, srcs, dst):
@@ -224,10 +238,37 @@ def ssd_mobilenet(width_div=1, in_hw=300, n_class=91):
                  (3, in_hw, in_hw), "uniform", nodes, "y")
 
 
+def norm_residual(widths=(64, 128), blocks=1, groups=8, in_hw=32, n_class=10):
+    """A small network of residual blocks whose norms cannot be folded into the
+    convolutions: per width a strided 3x3 convolution, then ``blocks`` times
+    two 3x3 convolutions behind group norm + SiLU with the shortcut added, and
+    two per-pixel products (four times as wide inside, GELU) behind group norm
+    with the shortcut added; global average pool and a product at the end."""
+    nodes, src, C = [], "x", 3
+    for i, K in enumerate(widths):
+        t = lambda n, i=i: "w%d_%s" % (i, n)
+        nodes.append(_conv(t("down"), src, t("in"), C, K, 3, 2, 1, False))
+        src, C = t("in"), K
+        for b in range(blocks):
+            u = lambda n, i=i, b=b: "w%d_%d_%s" % (i, b, n)
+            nodes.append(_groupnorm(u("n1"), src, u("a1"), C, groups, "silu"))
+            nodes.append(_conv(u("c1"), u("a1"), u("b1"), C, C, 3, 1, 1, False))
+            nodes.append(_groupnorm(u("n2"), u("b1"), u("a2"), C, groups, "silu"))
+            nodes.append(_conv(u("c2"), u("a2"), u("b2"), C, C, 3, 1, 1, False, residual=src))
+            nodes.append(_groupnorm(u("n3"), u("b2"), u("a3"), C, groups))
+            nodes.append(_matmul(u("up"), u("a3"), u("h"), C, 4 * C, "gelu"))
+            nodes.append(_matmul(u("out"), u("h"), u("o"), 4 * C, C, residual=u("b2")))
+            src = u("o")
+    nodes.append(_groupnorm("norm", src, "n", C, groups, "relu", residual=src))
+    nodes.append(_gavg("pool", "n", "p"))
+    nodes.append(_matmul("head", "p", "y", C, n_class))
+    return Model("norm_residual_%s_%d_%d" % ("_".join(map(str, widths)), blocks, in_hw), (3, in_hw, in_hw), "normal", nodes, "y")
+
+
 def parameters(model, seed=0):
     """Seeded weights and biases of ``model``: ``{node name: (w, b)}`` with
     ``w`` in the canonical (K, C, R, S) / (Out, In) order, bfloat16-exact
-    float32, and ``b`` float32."""
+    float32, and ``b`` float32; of a group norm its scale and shift, float32."""
     out = {}
     for nd in model.nodes:
         if nd.op == "conv":
@@ -238,6 +279,12 @@ def parameters(model, seed=0):
             shape = (a["C"], 1, a["k"], a["k"])
         elif nd.op == "fc":
             shape = (nd.attr["Out"], nd.attr["In"])
+        elif nd.op == "matmul":
+            shape = (nd.attr["K"], nd.attr["C"])
+        elif nd.op == "groupnorm":   # scale and shift
+            tag = "%s/%s" % (model.name, nd.name)
+            out[nd.name] = (1.0 + inputs.bias(seed, tag + ".w", nd.attr["C"]), inputs.bias(seed, tag + ".b", nd.attr["C"]))
+            continue
         else:
             continue
         tag = "%s/%s" % (model.name, nd.name)
