@@ -41,7 +41,8 @@ __device__ __forceinline__ float gelu(float v) {
 //   GATE    silu, gelu_tanh: v / (1 + exp(-s)) with s = v, or, as (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)),
 //           s = 2 sqrt(2 / pi) (v + 0.044715 v^3)
 //   NORMAL  gelu
-enum class ActCode { LINEAR, GATE, NORMAL };
+//   SILU    silu alone, four operations shorter than GATE, for kernels that the vector units bound
+enum class ActCode { LINEAR, GATE, NORMAL, SILU };
 inline ActCode act_code(int act) {
     return act == GPULET_ACT_GELU ? ActCode::NORMAL : act >= GPULET_ACT_SILU ? ActCode::GATE : ActCode::LINEAR;
 }
@@ -52,6 +53,9 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
     if constexpr (A == ActCode::NORMAL) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
+    } else if constexpr (A == ActCode::SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gate(v[i], v[i]);
     } else if constexpr (A == ActCode::GATE) {
         const float k1 = act == GPULET_ACT_SILU ? 1.f : 1.59576912f, k3 = act == GPULET_ACT_SILU ? 0.f : 1.59576912f * 0.044715f;
 #pragma unroll

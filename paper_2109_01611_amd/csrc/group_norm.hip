@@ -3,7 +3,7 @@
 // with mean and var over the H x W x C / groups values of an image's group of channels.  Statistics are in fp32, the
 // variance as the mean square of the differences from a mean (not of the values, which loses it where the mean is large).
 //
-// Bound by memory: x is read once and y written once, with about 20 vector operations an element.  Two forms:
+// Bound by memory: x is read once and y written once, with about 14 vector operations an element.  Two forms:
 //
 // * held: a workgroup keeps whole groups of one image in registers: one launch, x read once.  For up to kHeldBytes.
 // * two launches for larger groups: the first reduces chunks of an image to (mean, sum of squared differences) per group,
@@ -182,7 +182,7 @@ __device__ __forceinline__ typename RawUnit<V * sizeof(T)>::Type finish_unit(con
     float f[V];
     unpack<T, V>(x, f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = (f[i] - mean) * a[i] + b[i];
+    for (int i = 0; i < V; ++i) f[i] = (f[i] - mean) * a[i] + b[i];   // the shift minus mean * a would lose what is near the mean
     if (res) {
         float g[V];
         unpack<T, V>(r, g);
@@ -631,6 +631,7 @@ hipError_t launch_type(const Plan &pl, hipStream_t stream) {
 
 template <typename T>
 hipError_t launch_act(const Plan &pl, hipStream_t stream) {
+    if (pl.p.act == GPULET_ACT_SILU) return launch_type<T, ActCode::SILU>(pl, stream);
     switch (act_code(pl.p.act)) {
         case ActCode::NORMAL: return launch_type<T, ActCode::NORMAL>(pl, stream);
         case ActCode::GATE: return launch_type<T, ActCode::GATE>(pl, stream);

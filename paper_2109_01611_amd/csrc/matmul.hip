@@ -4,15 +4,17 @@
 // layer cannot stand for: wide activations, fp16, fp32 results, rows that are slices of wider ones, any number of rows.
 //
 // Forms, chosen per call by an estimate of their times (choose_form):
-//   direct   few rows or few tiles: operands go from memory straight into the matrix instructions, the depth is shared by
-//            the wavefronts of a workgroup.  Bound by memory: 1 x 4096 x 4096 8.3 us (4.0 TB/s of the weights).
-//   tile     64x64, 128x64 and 128x128 tiles, operands staged in LDS by transfers that pass no register.  Bound by the
-//            rate at which a CU takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128
-//            56 us, 933 TFLOP/s.  The 64x64 and 128x128 ones also with a depth that up to eight workgroups share, whose
-//            sums meet in the workspace.
+//   ring     up to 64x64 of y a workgroup, whose wavefronts share the depth, each with slices of its own in LDS and no barrier
+//            before the end.  Few rows, few tiles.  Bound by memory: 1 x 4096 x 4096 7.5 us (4.5 TB/s of the weights),
+//            24 x 1024 x 4096 4.9, 197 x 1024 x 4096 8.7.
+//   tile     64x64, 128x64 and 128x128 tiles that a workgroup goes through slice by slice.  Bound by the rate at which a CU
+//            takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128 56 us, 933 TFLOP/s.
+//            The 64x64 one also with a depth that up to eight workgroups share, whose sums meet in the workspace: tall y with
+//            few tiles and a long depth (5470 x 88 x 2504 15.9 us, in rings 18.4).
 //   big      256x256 tiles, 160 KB of LDS: as many matrix instructions as transfers can feed.  8192 x 4096 x 4096 216 us,
 //            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 1.33.
-//   staged   64x64 tiles whose operands pass through registers: rows that do not start at multiples of 16 bytes.
+//   direct,  rows that do not start at multiples of 16 bytes or a depth that is not a multiple of 8: operands go from memory
+//   staged   into the matrix instructions (few rows, few tiles), or through registers into LDS (64x64 tiles).
 //            2048 x 1024 x 1001 19 us.
 #include <hip/hip_runtime.h>
 
@@ -47,7 +49,8 @@ struct Params {
     int tiles_m, tiles_n;
     int total, per_die;     // workgroups, and a die's share of them
     int splits;             // workgroups that share a tile
-    int slices;             // slices of the depth: of 64, a workgroup's (splits > 1); of 32, a wavefront's (direct)
+    int slices;             // slices of the depth: of 64, a workgroup's (splits > 1) or a wavefront's (ring); of 32, a
+                            // wavefront's (direct)
     float *part;            // splits > 1: [split][M][N] sums
     int vec;                // rows of y and the residual allow 16-byte accesses
     FastDiv d_tiles, d_tiles_n, d_tiles_m;
@@ -107,40 +110,39 @@ __device__ __forceinline__ void load_bias(const Params &p, int n, float (&b)[NC]
     for (int i = 0; i < NC; ++i) b[i] = p.b && n + i < p.N ? p.b[n + i] : 0.f;
 }
 
-// Elements [k, k + 8) of a row, all of them in it.  ODD: the row may start at any element; a load that is not aligned to 4
-// bytes takes several times as long (787 x 333 x 1001 18.5 us, x 1002 8.0), so 20 bytes from the 4-byte boundary before are
-// loaded and shifted.  The first and the last 2 bytes then belong to no element of the eight; they lie in the same aligned 4
-// bytes as one that does.
-template <bool ODD, typename T>
-__device__ __forceinline__ uint4 load_whole(const T *row, int k) {
-    uint4 v;
-    if constexpr (ODD) {
-        const unsigned long long at = reinterpret_cast<unsigned long long>(row + k);
-        const unsigned shift = (static_cast<unsigned>(at) & 2u) * 8u;
-        const unsigned *q = reinterpret_cast<const unsigned *>(at & ~3ull);
-        __builtin_memcpy(&v, q, 16);
-        const unsigned last = q[shift ? 4 : 3];
-        v.x = __builtin_amdgcn_alignbit(v.y, v.x, shift);
-        v.y = __builtin_amdgcn_alignbit(v.z, v.y, shift);
-        v.z = __builtin_amdgcn_alignbit(v.w, v.z, shift);
-        v.w = __builtin_amdgcn_alignbit(last, v.w, shift);
-    } else {
-        __builtin_memcpy(&v, row + k, 16);
-    }
-    return v;
-}
-
 // Elements [k, k + 8) of a row; zero from K on.
-template <bool ODD, typename T>
+template <typename T>
 __device__ __forceinline__ uint4 load_cut(const T *row, int k, int K) {
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (k + 8 <= K) return load_whole<ODD>(row, k);
     if (k >= K) return v;
+    if (k + 8 <= K) {
+        __builtin_memcpy(&v, row + k, 16);
+        return v;
+    }
     unsigned short e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = k + i < K ? reinterpret_cast<const unsigned short *>(row)[k + i] : 0;
     __builtin_memcpy(&v, e, 16);
     return v;
+}
+
+// Rows that may start at any element: a load that is not aligned to 4 bytes takes several times as long (787 x 333 x 1001
+// 18.5 us, x 1002 8.0).  Instead 16 bytes are loaded from the 4-byte boundary at or before `at`, the dword behind them is
+// taken from the lane that loaded the next 16 bytes of the row or loaded (`tail`), and the five are shifted.  2 of the bytes
+// loaded may lie outside of the eight elements, in the same aligned 4 bytes as one of them.
+__device__ __forceinline__ uint4 load_floor(const void *at) {
+    uint4 v;
+    __builtin_memcpy(&v, reinterpret_cast<const void *>(reinterpret_cast<unsigned long long>(at) & ~3ull), 16);
+    return v;
+}
+__device__ __forceinline__ unsigned load_tail(const void *at) {   // the dword behind load_floor's, if it is needed
+    const unsigned long long a = reinterpret_cast<unsigned long long>(at);
+    return reinterpret_cast<const unsigned *>(a & ~3ull)[a & 2 ? 4 : 3];
+}
+__device__ __forceinline__ uint4 shift_in(const uint4 &v, unsigned behind, const void *at) {
+    const unsigned shift = (static_cast<unsigned>(reinterpret_cast<unsigned long long>(at)) & 2u) * 8u;
+    return make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, shift), __builtin_amdgcn_alignbit(v.z, v.y, shift),
+                      __builtin_amdgcn_alignbit(v.w, v.z, shift), __builtin_amdgcn_alignbit(behind, v.w, shift));
 }
 
 // ---- rows that start anywhere
@@ -166,11 +168,32 @@ __global__ __launch_bounds__(256) void staged_kernel(Params p) {
         wr[i] = static_cast<const T *>(p.w) + static_cast<long long>(wok[i] ? n : 0) * p.ldw;
     }
     uint4 xs[2], ws[2];
+    unsigned xt[2] = {}, wt[2] = {};   // ODD: the dword behind, where the next lane does not have it
+    auto request = [&](const T *r, int k, int K, uint4 &v, unsigned &tail) {
+        if constexpr (!ODD) {
+            v = load_cut(r, k, K);
+        } else if (k + 8 <= K) {
+            v = load_floor(r + k);
+            if (q == 7 || k + 16 > K) tail = load_tail(r + k);
+        } else {
+            v = load_cut(r, k, K);
+        }
+    };
+    // What the loads brought as it goes into LDS.
+    auto arrived = [&](const T *r, int k, int K, const uint4 &v, unsigned tail) {
+        if constexpr (!ODD) {
+            return v;
+        } else {
+            unsigned behind = __builtin_amdgcn_update_dpp(0, static_cast<int>(v.x), 0x101, 0xf, 0xf, true);   // of the next lane
+            if (q == 7 || k + 16 > K) behind = tail;
+            return k + 8 <= K ? shift_in(v, behind, r + k) : v;
+        }
+    };
     auto fetch = [&](int k) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            xs[i] = load_cut<ODD>(xr[i], k + 8 * q, xok[i] ? p.K : 0);
-            ws[i] = load_cut<ODD>(wr[i], k + 8 * q, wok[i] ? p.K : 0);
+            request(xr[i], k + 8 * q, xok[i] ? p.K : 0, xs[i], xt[i]);
+            request(wr[i], k + 8 * q, wok[i] ? p.K : 0, ws[i], wt[i]);
         }
     };
     f32x4 acc[2][2] = {};
@@ -180,8 +203,8 @@ __global__ __launch_bounds__(256) void staged_kernel(Params p) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = (row + 32 * i) * 8 + (q ^ ((row >> 1) & 7));
-            tile[0][at] = xs[i];
-            tile[1][at] = ws[i];
+            tile[0][at] = arrived(xr[i], k + 8 * q, xok[i] ? p.K : 0, xs[i], xt[i]);
+            tile[1][at] = arrived(wr[i], k + 8 * q, wok[i] ? p.K : 0, ws[i], wt[i]);
         }
         __syncthreads();
         if (k + 64 < p.K) fetch(k + 64);
@@ -487,7 +510,29 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
     }
 }
 
-// ---- few rows or few tiles: no LDS in the main loop
+// ---- few rows or few tiles of rows that start anywhere: no LDS in the main loop
+
+// Eight elements each at row, row + 32, ...: lane l has chunk l / 16 of the 32 elements.
+template <bool ODD, typename T, int U>
+__device__ __forceinline__ void load_run(const T *row, uint4 (&v)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if constexpr (ODD) v[u] = load_floor(row + 32 * u);
+        else __builtin_memcpy(&v[u], row + 32 * u, 16);
+    }
+}
+// The chunk behind a lane's is 16 lanes on, or in the first lanes' next element.
+template <typename T, int U>
+__device__ __forceinline__ void shift_run(const T *row, uint4 (&v)[U], unsigned tail) {
+    const int lane = threadIdx.x & 63, from = ((lane + 16) & 63) * 4;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned give = lane >= 16 ? v[u].x : u + 1 < U ? v[u + 1].x : 0u;
+        unsigned behind = __builtin_amdgcn_ds_bpermute(from, static_cast<int>(give));
+        if (u + 1 == U && lane >= 48) behind = tail;
+        v[u] = shift_in(v[u], behind, row);
+    }
+}
 
 // 16 MB rows by 16 NB columns of y a workgroup, its wavefronts each with a range of the depth and operands straight from
 // memory into the matrix instructions; their sums meet in LDS.  Rows may start at any element.  A wavefront has U steps of 32
@@ -512,29 +557,39 @@ __global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
     f32x4 acc[MB][NB] = {};
     int k = k0 + 8 * (lane >> 4);
     for (; k - 8 * (lane >> 4) + 32 * U <= k1; k += 32 * U) {
-        uint4 a[U][NB], b[U][MB];
+        uint4 a[NB][U], b[MB][U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int j = 0; j < NB; ++j) load_run<ODD>(wr[j] + k, a[j]);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) a[u][j] = load_whole<ODD>(wr[j], k + 32 * u);
+        for (int i = 0; i < MB; ++i) load_run<ODD>(xr[i] + k, b[i]);
+        if constexpr (ODD) {
+            unsigned wtail[NB] = {}, xtail[MB] = {};
+            if (lane >= 48) {   // the last chunk of the run
 #pragma unroll
-            for (int i = 0; i < MB; ++i) b[u][i] = load_whole<ODD>(xr[i], k + 32 * u);
+                for (int j = 0; j < NB; ++j) wtail[j] = load_tail(wr[j] + k + 32 * (U - 1));
+#pragma unroll
+                for (int i = 0; i < MB; ++i) xtail[i] = load_tail(xr[i] + k + 32 * (U - 1));
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) shift_run(wr[j] + k, a[j], wtail[j]);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) shift_run(xr[i] + k, b[i], xtail[i]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[u][j], b[u][i], acc[i][j], T());
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[j][u], b[i][u], acc[i][j], T());
     }
     if (k - 8 * (lane >> 4) < k1) {   // the rest, its last chunk perhaps short
         uint4 a[U][NB], b[U][MB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int j = 0; j < NB; ++j) a[u][j] = load_cut<ODD>(wr[j], k + 32 * u, k1);
+            for (int j = 0; j < NB; ++j) a[u][j] = load_cut(wr[j], k + 32 * u, k1);
 #pragma unroll
-            for (int i = 0; i < MB; ++i) b[u][i] = load_cut<ODD>(xr[i], k + 32 * u, k1);
+            for (int i = 0; i < MB; ++i) b[u][i] = load_cut(xr[i], k + 32 * u, k1);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -552,6 +607,96 @@ __global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
         f32x4 s = sums[0][item];
 #pragma unroll
         for (int i = 1; i < WAVES; ++i) s += sums[i][item];
+        const int blk = item >> 6, l = item & 63;
+        const int m = m0 + 16 * (blk / NB) + (l & 15), n = n0 + 16 * (blk % NB) + 4 * (l >> 4);
+        if (m >= p.M || n >= p.N) continue;
+        float v[4] = {s[0], s[1], s[2], s[3]}, bias[4];
+        load_bias(p, n, bias);
+        finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
+    }
+}
+
+// ---- few rows or few tiles
+
+// 16 MB rows by 16 NB columns of y a workgroup, its wavefronts each with a range of the depth and a ring of RING slices of 64
+// in LDS that nobody else touches: no barrier until their sums meet.  Transfers as in the tile kernels: 8 lanes bring 128
+// consecutive bytes of a row, where the matrix instructions' own layout would have 16 lanes ask for 16 rows at once (operands
+// straight from memory: 24 x 1024 x 4096 9.1 us instead of 4.9, 197 x 1024 x 4096 17.2 instead of 8.7).
+template <typename T, typename TO, ActCode A, int MB, int NB, int WAVES, int RING>
+__global__ __launch_bounds__(64 * WAVES) void ring_kernel(Params p) {
+    constexpr int PIECES = 2 * (MB + NB), ITEMS = MB * NB * 64, SLOT = PIECES * 1024, LDS = RING * SLOT * WAVES;
+    constexpr int SUMS = WAVES * ITEMS * 16;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS > SUMS ? LDS : SUMS];
+    const int id = die_block(p.per_die, blockIdx.x);
+    if (id >= p.total) return;
+    const int tn = fdiv(id, p.d_tiles_m), tm = id - tn * p.tiles_m;   // the row blocks of a column block next to one another
+    const int m0 = tm * 16 * MB, n0 = tn * 16 * NB;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int mrows = min(16 * MB, p.M - m0), nrows = min(16 * NB, p.N - n0);
+    const i32x4 xs = make_rsrc(static_cast<const T *>(p.x) + static_cast<long long>(m0) * p.ldx, 2u * ((mrows - 1) * p.ldx + p.K));
+    const i32x4 ws = make_rsrc(static_cast<const T *>(p.w) + static_cast<long long>(n0) * p.ldw, 2u * ((nrows - 1) * p.ldw + p.K));
+    const int k0 = wave * p.slices * 64, k1 = min(p.K, k0 + p.slices * 64), n_slices = k1 > k0 ? (k1 - k0 + 63) >> 6 : 0;
+    unsigned voff[PIECES];
+    const int q = lane & 7;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+        const int row = 8 * (j < 2 * MB ? j : j - 2 * MB) + (lane >> 3), chunk = q ^ ((row >> 1) & 7);
+        voff[j] = row < (j < 2 * MB ? mrows : nrows) ? static_cast<unsigned>(row * (j < 2 * MB ? p.ldx : p.ldw) + chunk * 8) * 2u : OOB;
+    }
+    unsigned char *mine = lds + wave * RING * SLOT;
+    const unsigned base = lds_addr(lds) + wave * RING * SLOT;
+    auto fetch = [&](int s, int at) {
+        const int k = k0 + s * 64;
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            unsigned v = voff[j];
+            if (k + 64 > p.K) {
+                const int row = 8 * (j < 2 * MB ? j : j - 2 * MB) + (lane >> 3);
+                if (k + 8 * (q ^ ((row >> 1) & 7)) >= p.K) v = OOB;
+            }
+            dma16(j < 2 * MB ? xs : ws, base + at * SLOT + j * 1024, v, k * 2);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < RING; ++i)
+        if (i < n_slices) fetch(i, i);
+    f32x4 acc[MB][NB] = {};
+    const int fr = lane & 15, key = (fr >> 1) & 7;
+    const int c0 = ((lane >> 4) ^ key) * 16, c1 = ((4 + (lane >> 4)) ^ key) * 16;
+    int at = 0;
+    for (int s = 0; s < n_slices; ++s) {
+        if (s + RING <= n_slices) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PIECES * (RING - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const unsigned char *buf = mine + at * SLOT + fr * 128;
+        uint4 a[2][NB], b[2][MB];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) a[h][j] = *reinterpret_cast<const uint4 *>(buf + (MB + j) * 2048 + (h ? c1 : c0));
+#pragma unroll
+            for (int i = 0; i < MB; ++i) b[h][i] = *reinterpret_cast<const uint4 *>(buf + i * 2048 + (h ? c1 : c0));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read before it is filled again
+        if (s + RING < n_slices) fetch(s + RING, at);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[h][j], b[h][i], acc[i][j], T());
+        at = at + 1 == RING ? 0 : at + 1;
+    }
+    __syncthreads();   // nothing is on its way any more
+    f32x4 *sums = reinterpret_cast<f32x4 *>(lds);
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[wave * ITEMS + (i * NB + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int item = threadIdx.x; item < ITEMS; item += 64 * WAVES) {
+        f32x4 s = sums[item];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s += sums[i * ITEMS + item];
         const int blk = item >> 6, l = item & 63;
         const int m = m0 + 16 * (blk / NB) + (l & 15), n = n0 + 16 * (blk % NB) + 4 * (l >> 4);
         if (m >= p.M || n >= p.N) continue;
@@ -589,48 +734,57 @@ __global__ __launch_bounds__(256) void join_kernel(Params p) {
 
 // ---- host side
 
-enum Form { DIRECT4, DIRECT8, DIRECT22, TILE64, TILE128x64, TILE128, BIG, STAGED };
+enum Form { RING11, RING11W, RING12, RING22, RING42, RING44, TILE64, TILE128x64, TILE128, BIG, DIRECT, DIRECT22, STAGED };
 
-// Microseconds of a form as fitted to 90 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192 (the fastest
-// of the forms 4 % faster than the one chosen, geometric mean):
-//   start + (slices a CU goes through, one after the other) * (time of a slice) + (tiles of the busiest CU) * finish
-// where a slice takes `alone` when it has the CU for itself and `busy` times the workgroups that share it.
+// Microseconds of the forms, fitted to 130 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192 (what is
+// chosen takes 3 % longer than the fastest form, geometric mean).  A CU takes its share of the workgroups in rounds of
+// `resident`; a round costs `round`.  A slice of a tile takes `near` + `far` * (how much of 8 MB the operands are: from the
+// caches or from memory) when it has the CU for itself, and `busy` times the workgroups that share the CU if that is longer.
+// `finish`: the epilogue of a workgroup.
 struct TileCost {
     int bm, bn, resident;
-    double start, alone, busy, finish;
+    double round, near, far, busy, finish;
 };
-constexpr TileCost kTile64 = {64, 64, 5, 2.4, 0.32, 0.24, 0.46}, kTile128x64 = {128, 64, 3, 2.2, 0.46, 0.35, 1.0},
-                   kTile128 = {128, 128, 2, 1.2, 0.62, 0.48, 3.2}, kBig = {256, 256, 1, 1.0, 1.27, 1.27, 5.7},
-                   kStaged = {64, 64, 5, 2.5, 0.70, 0.26, 0.46};
-// A direct form takes what its operands take at `per_kb` or its batches of loads one after the other, whichever is longer.
-struct DirectCost {
+constexpr TileCost kTile64 = {64, 64, 5, 0.5, 0.0, 0.46, 0.25, 0.45}, kTile128x64 = {128, 64, 3, 0.0, 0.38, 0.16, 0.325, 1.36},
+                   kTile128 = {128, 128, 2, 0.0, 0.44, 0.29, 0.44, 3.2}, kBig = {256, 256, 1, 4.0, 1.35, 0.1, 1.45, 6.0},
+                   kStaged = {64, 64, 5, 0.5, 0.50, 0.10, 0.29, 0.46};
+// The wavefronts of a ring or direct form work side by side on slices of 64; a round takes as long as its slices one after the
+// other or as its operands at `per_kb`.
+struct RingCost {
     int mb, nb, waves, resident;
-    double start, batch, per_kb;
+    double round, near, far, per_kb, finish;
 };
-constexpr DirectCost kDirect4 = {1, 1, 4, 8, 2.4, 0.48, 0.022}, kDirect8 = {1, 1, 8, 4, 2.4, 0.62, 0.023},
-                     kDirect22 = {2, 2, 8, 2, 2.0, 1.47, 0.027};
+constexpr RingCost kRing11 = {1, 1, 4, 2, 0.1, 0.17, 0.06, 0.0142, 0.36}, kRing11W = {1, 1, 16, 1, 0.45, 0.16, 0.77, 0.0072, 0.44},
+                   kRing12 = {1, 2, 8, 1, 0.32, 0.10, 0.63, 0.0079, 0.61}, kRing22 = {2, 2, 4, 2, 0.0, 0.27, 0.09, 0.014, 0.68},
+                   kRing42 = {4, 2, 4, 1, 0.07, 0.37, 0.09, 0.0175, 1.15}, kRing44 = {4, 4, 4, 1, 1.8, 0.06, 0.56, 0.0172, 0.35},
+                   kDirect = {1, 1, 8, 4, 0.2, 0.31, 0.0, 0.021, 0.0}, kDirect22 = {2, 2, 8, 2, 0.0, 0.73, 0.0, 0.027, 0.0};
+constexpr double kStart = 2.2;
 // The launch that joins a shared depth: itself and what the host needs for it, and its traffic by the megabyte.
-constexpr double kJoin = 4.5, kJoinMb = 0.35;
+constexpr double kJoin = 4.9, kJoinMb = 0.34;
 constexpr int kMaxSplit = 8;
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+double from_memory(const MatmulArgs &a) { return std::min(1.0, (1.0 * a.M + a.N) * a.K * 2.0 / 8e6); }
+
 double tile_cost(const TileCost &c, const MatmulArgs &a, int split, int n_cu) {
     const double tiles = 1.0 * ceil_div(a.M, c.bm) * ceil_div(a.N, c.bn) * split;
     const int n = static_cast<int>((tiles + n_cu - 1) / n_cu), slices = ceil_div(ceil_div(a.K, 64), split);
-    auto slice = [&](int wgs) { return std::max(c.alone, c.busy * wgs); };
+    const double alone = c.near + c.far * from_memory(a);
+    auto round = [&](int wgs) { return c.round + slices * std::max(alone, c.busy * wgs); };
     const int rest = n % c.resident;
-    double t = c.start + slices * (n / c.resident * slice(c.resident) + (rest ? slice(rest) : 0.0)) + c.finish * n;
+    double t = kStart + n / c.resident * round(c.resident) + (rest ? round(rest) : 0.0) + c.finish * n;
     if (split > 1) t += kJoin + kJoinMb * 4e-6 * split * a.M * a.N;
     return t;
 }
 
-double direct_cost(const DirectCost &c, const MatmulArgs &a, int n_cu, double slower) {
+double ring_cost(const RingCost &c, const MatmulArgs &a, int n_cu, double slower = 1.0) {
     const double wgs = 1.0 * ceil_div(a.M, 16 * c.mb) * ceil_div(a.N, 16 * c.nb);
     if (wgs > (1 << 20)) return 1e30;   // grids stay below 2^32 threads
-    const int n = static_cast<int>((wgs + n_cu - 1) / n_cu);
+    const int n = static_cast<int>((wgs + n_cu - 1) / n_cu), rounds = ceil_div(n, c.resident);
     const double kb = (std::min(a.M, 16 * c.mb) + std::min(a.N, 16 * c.nb)) * (a.K * 2.0 / 1024);
-    return c.start + slower * std::max(1.0 * ceil_div(n, c.resident) * ceil_div(a.K, 128 * c.waves) * c.batch, n * kb * c.per_kb);
+    const double chain = 1.0 * rounds * ceil_div(ceil_div(a.K, 64), c.waves) * (c.near + c.far * from_memory(a));
+    return kStart + rounds * c.round + slower * std::max(chain, n * kb * c.per_kb) + c.finish * n;
 }
 
 struct Choice {
@@ -649,24 +803,36 @@ Choice choose_form(const MatmulArgs &a, bool rows16, bool odd, int n_cu, size_t 
             best = Choice{f, split};
         }
     };
-    const double slower = odd ? 1.5 : rows16 ? 1.0 : 1.2;
-    consider(DIRECT4, 1, direct_cost(kDirect4, a, n_cu, slower));
-    consider(DIRECT8, 1, direct_cost(kDirect8, a, n_cu, slower));
-    consider(DIRECT22, 1, direct_cost(kDirect22, a, n_cu, slower));
     if (!rows16) {
-        consider(STAGED, 1, tile_cost(kStaged, a, 1, n_cu));
+        // odd rows: 787 x 333 x 1001 direct 9.8 us and staged 19.1, x 1002 8.0 and 13.5; 8192 x 2047 x 2047 staged 200 us,
+        // 8192 x 2048 x 2046 155
+        consider(DIRECT, 1, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
+        consider(DIRECT22, 1, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
+        consider(STAGED, 1, (odd ? 1.4 : 1.0) * tile_cost(kStaged, a, 1, n_cu));
         return best;
     }
-    consider(TILE64, 1, tile_cost(kTile64, a, 1, n_cu));
-    consider(TILE128x64, 1, tile_cost(kTile128x64, a, 1, n_cu));
-    consider(TILE128, 1, tile_cost(kTile128, a, 1, n_cu));
-    consider(BIG, 1, tile_cost(kBig, a, 1, n_cu));
-    const size_t plane = 4ull * a.M * a.N;
-    if (plane >= (1ull << 32)) return best;
-    for (int split = 2; split <= kMaxSplit && split * plane <= ws_bytes && split <= ceil_div(a.K, 64); split *= 2) {
-        consider(TILE64, split, tile_cost(kTile64, a, split, n_cu));
-        consider(TILE128, split, tile_cost(kTile128, a, split, n_cu));
+    // Forms that cannot be the fastest are not looked at: an estimate costs the host 30 ns.
+    const double tiles = 1.0 * ceil_div(a.M, 64) * ceil_div(a.N, 64);
+    if (tiles <= 3.0 * n_cu) {
+        consider(RING11, 1, ring_cost(kRing11, a, n_cu));
+        consider(RING11W, 1, ring_cost(kRing11W, a, n_cu));
+        consider(RING12, 1, ring_cost(kRing12, a, n_cu));
+        if (a.M > 16) {
+            consider(RING22, 1, ring_cost(kRing22, a, n_cu));
+            consider(RING42, 1, ring_cost(kRing42, a, n_cu));
+            consider(RING44, 1, ring_cost(kRing44, a, n_cu));
+        }
     }
+    if (a.M > 16) consider(TILE64, 1, tile_cost(kTile64, a, 1, n_cu));
+    if (tiles >= n_cu) {
+        consider(TILE128x64, 1, tile_cost(kTile128x64, a, 1, n_cu));
+        consider(TILE128, 1, tile_cost(kTile128, a, 1, n_cu));
+    }
+    if (tiles >= 4.0 * n_cu) consider(BIG, 1, tile_cost(kBig, a, 1, n_cu));
+    const size_t plane = 4ull * a.M * a.N;
+    if (a.M <= 16 || tiles > 2.0 * n_cu || plane >= (1ull << 32)) return best;
+    for (int split = 2; split <= kMaxSplit && split * plane <= ws_bytes && split <= ceil_div(a.K, 64); split *= 2)
+        consider(TILE64, split, tile_cost(kTile64, a, split, n_cu));
     return best;
 }
 
@@ -696,13 +862,20 @@ void launch_tile(Params &p, hipStream_t stream) {
     tile_kernel<T, TO, A, BM, BN, 2, 2, false><<<grid, 256, 0, stream>>>(p);
 }
 
-template <typename T, typename TO, ActCode A, int BM, int BN>
+template <typename T, typename TO, ActCode A, int MB, int NB, int WAVES, int RING>
+void launch_ring(Params &p, hipStream_t stream) {
+    const dim3 grid = set_grid<16 * MB, 16 * NB>(p);
+    p.slices = ceil_div(ceil_div(p.K, 64), WAVES);
+    ring_kernel<T, TO, A, MB, NB, WAVES, RING><<<grid, 64 * WAVES, 0, stream>>>(p);
+}
+
+template <typename T, typename TO, ActCode A>
 hipError_t launch_split(Params &p, hipStream_t stream) {
     const int slices = ceil_div(p.K, 64);
     p.slices = ceil_div(slices, p.splits);
     p.splits = ceil_div(slices, p.slices);   // none without a slice
-    const dim3 grid = set_grid<BM, BN>(p);
-    tile_kernel<T, float, ActCode::LINEAR, BM, BN, 2, 2, true><<<grid, 256, 0, stream>>>(p);
+    const dim3 grid = set_grid<64, 64>(p);
+    tile_kernel<T, float, ActCode::LINEAR, 64, 64, 2, 2, true><<<grid, 256, 0, stream>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const size_t threads = static_cast<size_t>(p.M) * ceil_div(p.N, 4);
@@ -712,11 +885,15 @@ hipError_t launch_split(Params &p, hipStream_t stream) {
 
 template <typename T, typename TO, ActCode A>
 hipError_t launch_act(Params &p, const Choice &c, bool odd, hipStream_t stream) {
-    if (p.splits > 1)
-        return c.form == TILE64 ? launch_split<T, TO, A, 64, 64>(p, stream) : launch_split<T, TO, A, 128, 128>(p, stream);
+    if (p.splits > 1) return launch_split<T, TO, A>(p, stream);
     switch (c.form) {
-        case DIRECT4: launch_direct<T, TO, A, 1, 1, 4>(p, odd, stream); break;
-        case DIRECT8: launch_direct<T, TO, A, 1, 1, 8>(p, odd, stream); break;
+        case RING11: launch_ring<T, TO, A, 1, 1, 4, 4>(p, stream); break;
+        case RING11W: launch_ring<T, TO, A, 1, 1, 16, 2>(p, stream); break;
+        case RING12: launch_ring<T, TO, A, 1, 2, 8, 3>(p, stream); break;
+        case RING22: launch_ring<T, TO, A, 2, 2, 4, 2>(p, stream); break;
+        case RING42: launch_ring<T, TO, A, 4, 2, 4, 3>(p, stream); break;
+        case RING44: launch_ring<T, TO, A, 4, 4, 4, 2>(p, stream); break;
+        case DIRECT: launch_direct<T, TO, A, 1, 1, 8>(p, odd, stream); break;
         case DIRECT22: launch_direct<T, TO, A, 2, 2, 8>(p, odd, stream); break;
         case TILE64: launch_tile<T, TO, A, 64, 64>(p, stream); break;
         case TILE128x64: launch_tile<T, TO, A, 128, 64>(p, stream); break;
