@@ -44,14 +44,15 @@ struct Params {
     float eps;
     int threads;              // of a workgroup
     int gb, cb;               // groups and channels of a workgroup
-    int upx, ug;              // units of V channels per pixel of a workgroup and per group
+    int upx, ug;              // units of V channels per pixel of a workgroup and per group in it
+    int slices, gu;           // two launches: workgroups that share the channels of a group (gb = 1), units of a whole group
     int R, iters;             // pixels the threads cover at once, and how often (held)
     int lanes;                // threads that join the values of a group: a power of two up to 64, all groups at once if it can
     int n_cb;                 // workgroups side by side in the channels
     int chunks, chunk;        // two launches: chunks of an image and their pixels
     int stat_chunks, stat_chunk;   // normalising launch: the same of the launch before
     int total, per_die;       // workgroups, and a die's share of them
-    FastDiv d_upx, d_ug, d_ncb, d_chunks;
+    FastDiv d_upx, d_ug, d_ncb, d_chunks, d_slices;
 };
 
 template <int UB> struct RawUnit;
@@ -155,12 +156,12 @@ template <int V>
 struct Place {
     int row, c, group;   // c: first channel, counted from the workgroup's first
     bool in;
-    __device__ __forceinline__ Place(const Params &p) {
+    __device__ __forceinline__ Place(const Params &p, int slice = 0) {
         row = fdiv(threadIdx.x, p.d_upx);
         const int u = threadIdx.x - row * p.upx;
         c = u * V;
         group = fdiv(u, p.d_ug);
-        in = row < p.R;
+        in = row < p.R && (p.slices == 1 || slice * p.upx + u < p.gu);
     }
 };
 
@@ -326,10 +327,11 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     const int id = die_block(p.per_die, blockIdx.x);
     if (id >= p.total) return;
     const int t = fdiv(id, p.d_ncb), cblk = id - t * p.n_cb, n = fdiv(t, p.d_chunks), k = t - n * p.chunks;
-    const int c0 = cblk * p.cb, q0 = k * p.chunk, q1 = min(p.HW, q0 + p.chunk);
-    const Place<V> at(p);
+    const int gblk = fdiv(cblk, p.d_slices), slice = cblk - gblk * p.slices, sc = slice * p.upx * V;
+    const int c0 = gblk * p.cb + sc, q0 = k * p.chunk, q1 = min(p.HW, q0 + p.chunk);
+    const Place<V> at(p, slice);
     const Rsrc xs = make_rsrc(static_cast<const char *>(p.x) + (static_cast<size_t>(n) * p.HW * p.ldx + c0) * sizeof(T),
-                              (static_cast<unsigned>(p.HW - 1) * p.ldx + p.cb) * static_cast<unsigned>(sizeof(T)));
+                              (static_cast<unsigned>(p.HW - 1) * p.ldx + p.cb - sc) * static_cast<unsigned>(sizeof(T)));
     W w(p, at, q0, q1);
     typename W::Raw xv[W::B];
     w.load(xs, p.ldx, xv);
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
             v = join(v, Stat{part[0][j], part[1][j], part[2][j]});
         }
         v = join_lanes(v, p.lanes);
-        if (sub == 0) p.part[(static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.chunks + k] = make_float2(v.mean, v.m2);
+        if (sub == 0) p.part[((static_cast<size_t>(n) * p.G + gblk * p.gb + g) * p.chunks + k) * p.slices + slice] = make_float2(v.mean, v.m2);
     }
 }
 
@@ -388,12 +390,13 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
     const int id = die_block(p.per_die, blockIdx.x);
     if (id >= p.total) return;
     const int t = fdiv(id, p.d_ncb), cblk = id - t * p.n_cb, n = fdiv(t, p.d_chunks), k = t - n * p.chunks;
-    const int c0 = cblk * p.cb, q0 = k * p.chunk, q1 = min(p.HW, q0 + p.chunk);
-    const Place<V> at(p);
+    const int gblk = fdiv(cblk, p.d_slices), slice = cblk - gblk * p.slices, sc = slice * p.upx * V;
+    const int c0 = gblk * p.cb + sc, q0 = k * p.chunk, q1 = min(p.HW, q0 + p.chunk);
+    const Place<V> at(p, slice);
     const size_t px = static_cast<size_t>(n) * p.HW;
     auto image = [&](const void *q, int ld) {
         return make_rsrc(static_cast<const char *>(q) + (px * ld + c0) * sizeof(T),
-                         (static_cast<unsigned>(p.HW - 1) * ld + p.cb) * static_cast<unsigned>(sizeof(T)));
+                         (static_cast<unsigned>(p.HW - 1) * ld + p.cb - sc) * static_cast<unsigned>(sizeof(T)));
     };
     const Rsrc xs = image(p.x, p.ldx), ys = image(p.y, p.ldy), rs = p.r ? image(p.r, p.ldr) : xs;
     W w(p, at, q0, q1);
@@ -404,12 +407,14 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
     load_affine<V>(p, c0 + (at.in ? at.c : 0), a, b);
     const int sub = threadIdx.x & (p.lanes - 1);
     for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {
-        const float2 *q = p.part + (static_cast<size_t>(n) * p.G + cblk * p.gb + g) * p.stat_chunks;
+        const int parts = p.stat_chunks * p.slices;
+        const float2 *q = p.part + (static_cast<size_t>(n) * p.G + gblk * p.gb + g) * parts;
         Stat v{0.f, 0.f, 0.f};
-        for (int i = sub; i < p.stat_chunks; i += p.lanes) {
+        for (int i = sub; i < parts; i += p.lanes) {
             const float2 e = q[i];
-            const int first = i * p.stat_chunk;
-            v = join(v, Stat{static_cast<float>(min(p.HW - first, p.stat_chunk)) * static_cast<float>(p.cg), e.x, e.y});
+            const int chunk = fdiv(i, p.d_slices), first = chunk * p.stat_chunk;
+            const int units = p.slices == 1 ? p.gu : min(p.upx, p.gu - (i - chunk * p.slices) * p.upx);
+            v = join(v, Stat{static_cast<float>(min(p.HW - first, p.stat_chunk)) * static_cast<float>(units * V), e.x, e.y});
         }
         v = join_lanes(v, p.lanes);
         if (sub == 0) stat[g] = make_float2(v.mean, 1.f / __builtin_sqrtf(v.m2 / v.n + p.eps));
@@ -433,45 +438,6 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
     }
 }
 
-// One workgroup per image and group, element by element: groups of more than kMaxThreads units.
-template <typename T, ActCode A>
-__global__ __launch_bounds__(kMaxThreads) void wide_kernel(Params p) {
-    __shared__ float res1[kMaxGb], res2[kMaxGb];
-    const int n = fdiv(blockIdx.x, p.d_ncb), g = blockIdx.x - n * p.n_cb;
-    const size_t px = static_cast<size_t>(n) * p.HW;
-    const T *x = static_cast<const T *>(p.x) + px * p.ldx + g * p.cg;
-    const T *r = p.r ? static_cast<const T *>(p.r) + px * p.ldr + g * p.cg : nullptr;
-    T *y = static_cast<T *>(p.y) + px * p.ldy + g * p.cg;
-    const float inv = 1.f / (static_cast<float>(p.HW) * static_cast<float>(p.cg));
-    const float first = static_cast<float>(x[0]);
-    float mean = 0.f, rstd = 0.f;
-    for (int pass = 0; pass < 3; ++pass) {
-        float s = 0.f, t = 0.f;
-        for (int q = 0; q < p.HW; ++q) {
-            for (int c = threadIdx.x; c < p.cg; c += kMaxThreads) {
-                float v[1] = {static_cast<float>(x[q * p.ldx + c])};
-                if (pass == 0) {
-                    t += v[0] - first;
-                } else if (pass == 1) {
-                    t += (v[0] - mean) * (v[0] - mean);
-                } else {
-                    v[0] = (v[0] - mean) * (p.gamma ? rstd * p.gamma[g * p.cg + c] : rstd) + (p.beta ? p.beta[g * p.cg + c] : 0.f);
-                    if (r) v[0] += static_cast<float>(r[q * p.ldr + c]);
-                    activate<A>(v, p.act);
-                    y[q * p.ldy + c] = static_cast<T>(v[0]);
-                }
-            }
-            if ((q & 255) == 255) {   // short partial sums: fewer roundings of a large one
-                s += t;
-                t = 0.f;
-            }
-        }
-        s += t;
-        if (pass == 0) mean = first + group_sum(s, p, 0, nullptr, res1) * inv;
-        else if (pass == 1) rstd = 1.f / __builtin_sqrtf(group_sum(s, p, 0, nullptr, res2) * inv + p.eps);
-    }
-}
-
 // ---- host side
 
 // Bytes of the groups a workgroup holds, at most.  Above, too few workgroups read pieces of pixels too short for the memory
@@ -491,7 +457,7 @@ constexpr size_t kMinStats = 8 << 10, kMaxStats = 256 << 10, kMinApply = 8 << 10
 constexpr size_t kStreamBytes = 64 << 20;
 
 struct Plan {
-    enum Form { HELD, TWO, WIDE } form;
+    enum Form { HELD, TWO } form;
     int V, iters;
     bool stream_out;
     Params p, q;   // of the only or first launch, and of the second
@@ -502,24 +468,27 @@ void set_blocks(Params &p, int N, int per_image) {
     p.per_die = (p.total + 7) / 8;
 }
 
-void set_units(Params &p, int V, int gb, int threads) {
+void set_units(Params &p, int V, int gb, int slices, int threads) {
     p.threads = threads;
     p.gb = gb;
     p.cb = gb * p.cg;
-    p.upx = p.cb / V;
-    p.ug = p.cg / V;
+    p.slices = slices;
+    p.gu = p.cg / V;
+    p.ug = (p.gu + slices - 1) / slices;
+    p.upx = gb * p.ug;
     p.R = threads / p.upx;
     p.lanes = 64;
     while (p.lanes > 1 && p.lanes * gb > threads) p.lanes /= 2;
-    p.n_cb = p.G / gb;
+    p.n_cb = p.G / gb * slices;
+    p.d_slices = make_fastdiv(slices);
     p.d_upx = make_fastdiv(p.upx);
     p.d_ug = make_fastdiv(p.ug);
     p.d_ncb = make_fastdiv(p.n_cb);
 }
 
 // Chunks of about `piece` bytes, made of whole batches.
-void set_chunks(Params &p, int V, int unit_bytes, int gb, int threads, size_t block_bytes, size_t piece, int N) {
-    set_units(p, V, gb, threads);
+void set_chunks(Params &p, int V, int unit_bytes, int gb, int slices, int threads, size_t block_bytes, size_t piece, int N) {
+    set_units(p, V, gb, slices, threads);
     const int chunks = static_cast<int>(std::max<size_t>(1, block_bytes / piece));
     const int whole = p.R * batch_of(unit_bytes);
     p.chunk = ((p.HW + chunks - 1) / chunks + whole - 1) / whole * whole;
@@ -545,12 +514,6 @@ Plan make_plan(const GroupNormArgs &a) {
     p.chunks = 1;
     p.chunk = p.HW;
     p.d_chunks = make_fastdiv(1);
-    if (p.cg / V > kMaxThreads) {
-        pl.form = Plan::WIDE;
-        set_units(p, p.cg, 1, 1);
-        set_blocks(p, a.N, p.G);
-        return pl;
-    }
     const int unit_dwords = std::max(1, V * es / 4);
     const size_t group_bytes = static_cast<size_t>(p.HW) * p.cg * es;
     // groups side by side until a pixel's piece is 64 bytes, half a line
@@ -568,7 +531,7 @@ Plan make_plan(const GroupNormArgs &a) {
             if (iters * unit_dwords > (threads < kMaxThreads ? 8 : kHeldDwords)) continue;
             pl.form = Plan::HELD;
             pl.iters = p.iters = iters;
-            set_units(p, V, gb, threads);
+            set_units(p, V, gb, 1, threads);
             set_blocks(p, a.N, p.n_cb);
             return pl;
         }
@@ -582,14 +545,16 @@ Plan make_plan(const GroupNormArgs &a) {
         if (next > kMaxGb || next * p.cg / V > kMaxThreads) break;
         gb = next;
     }
-    const size_t block_bytes = static_cast<size_t>(p.HW) * gb * p.cg * es;
+    // a group of more units than a workgroup has threads is shared by several
+    const int slices = (p.cg / V + kMaxThreads - 1) / kMaxThreads;
+    const size_t block_bytes = static_cast<size_t>(p.HW) * gb * p.cg * es / slices;
     const size_t stats = std::min(kMaxStats, std::max(kMinStats, block_bytes / 32));
-    const size_t apply = std::min(kMaxApply, std::max(kMinApply, block_bytes * (p.G / gb) / 256));
+    const size_t apply = std::min(kMaxApply, std::max(kMinApply, block_bytes * slices * (p.G / gb) / 256));
     pl.stream_out = static_cast<size_t>(a.N) * p.HW * p.C * es >= kStreamBytes;
     pl.q = p;
-    const int fewest = (gb * p.cg / V + 63) / 64 * 64;   // threads of one row
-    set_chunks(p, V, V * es, gb, std::max(stats >= (64 << 10) ? 512 : 256, fewest), block_bytes, stats, a.N);
-    set_chunks(pl.q, V, V * es, gb, std::max(256, fewest), block_bytes, apply, a.N);
+    const int fewest = ((gb * p.cg / V + slices - 1) / slices + 63) / 64 * 64;   // threads of one row
+    set_chunks(p, V, V * es, gb, slices, std::max(stats >= (64 << 10) ? 512 : 256, fewest), block_bytes, stats, a.N);
+    set_chunks(pl.q, V, V * es, gb, slices, std::max(256, fewest), block_bytes, apply, a.N);
     pl.q.stat_chunks = p.chunks;
     pl.q.stat_chunk = p.chunk;
     return pl;
@@ -615,10 +580,6 @@ hipError_t launch_units(const Plan &pl, hipStream_t stream) {
 
 template <typename T, ActCode A>
 hipError_t launch_type(const Plan &pl, hipStream_t stream) {
-    if (pl.form == Plan::WIDE) {
-        wide_kernel<T, A><<<dim3(pl.p.total), kMaxThreads, 0, stream>>>(pl.p);
-        return hipGetLastError();
-    }
     switch (pl.V) {
         case 8:
             if constexpr (sizeof(T) == 2) return launch_units<T, 8, A>(pl, stream);
@@ -652,7 +613,7 @@ hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream, int *la
 
 size_t group_norm_workspace(const GroupNormArgs &a) {
     const Plan pl = make_plan(a);
-    return pl.form == Plan::TWO ? static_cast<size_t>(a.N) * a.groups * pl.p.chunks * sizeof(float2) : 0;
+    return pl.form == Plan::TWO ? static_cast<size_t>(a.N) * a.groups * pl.p.chunks * pl.p.slices * sizeof(float2) : 0;
 }
 
 }  // namespace gpulet

@@ -3,7 +3,7 @@
 // for the per-pixel and per-row layers of a forward pass (paper Sec. 5) that a ReLU convolution or the fully connected
 // layer cannot stand for: wide activations, fp16, fp32 results, rows that are slices of wider ones, any number of rows.
 //
-// Forms, chosen per call by an estimate of their times (choose_form):
+// Forms, chosen per call by an estimate of their times (choose_matmul):
 //   ring     up to 64x64 of y a workgroup, whose wavefronts share the depth, each with slices of its own in LDS and no barrier
 //            before the end.  Few rows, few tiles.  Bound by memory: 1 x 4096 x 4096 7.5 us (4.5 TB/s of the weights),
 //            24 x 1024 x 4096 4.9, 197 x 1024 x 4096 8.7.
@@ -734,8 +734,6 @@ __global__ __launch_bounds__(256) void join_kernel(Params p) {
 
 // ---- host side
 
-enum Form { RING11, RING11W, RING12, RING22, RING42, RING44, TILE64, TILE128x64, TILE128, BIG, DIRECT, DIRECT22, STAGED };
-
 // Microseconds of the forms, fitted to 130 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192 (what is
 // chosen takes 3 % longer than the fastest form, geometric mean).  A CU takes its share of the workgroups in rounds of
 // `resident`; a round costs `round`.  A slice of a tile takes `near` + `far` * (how much of 8 MB the operands are: from the
@@ -754,7 +752,7 @@ struct RingCost {
     int mb, nb, waves, resident;
     double round, near, far, per_kb, finish;
 };
-constexpr RingCost kRing11 = {1, 1, 4, 2, 0.1, 0.17, 0.06, 0.0142, 0.36}, kRing11W = {1, 1, 16, 1, 0.45, 0.16, 0.77, 0.0072, 0.44},
+constexpr RingCost kRing11 = {1, 1, 4, 2, 0.1, 0.17, 0.06, 0.0142, 0.36}, kRing11W = {1, 1, 16, 1, 0.45, 0.16, 0.60, 0.0072, 0.44},
                    kRing12 = {1, 2, 8, 1, 0.32, 0.10, 0.63, 0.0079, 0.61}, kRing22 = {2, 2, 4, 2, 0.0, 0.27, 0.09, 0.014, 0.68},
                    kRing42 = {4, 2, 4, 1, 0.07, 0.37, 0.09, 0.0175, 1.15}, kRing44 = {4, 4, 4, 1, 1.8, 0.06, 0.56, 0.0172, 0.35},
                    kDirect = {1, 1, 8, 4, 0.2, 0.31, 0.0, 0.021, 0.0}, kDirect22 = {2, 2, 8, 2, 0.0, 0.73, 0.0, 0.027, 0.0};
@@ -787,53 +785,10 @@ double ring_cost(const RingCost &c, const MatmulArgs &a, int n_cu, double slower
     return kStart + rounds * c.round + slower * std::max(chain, n * kb * c.per_kb) + c.finish * n;
 }
 
-struct Choice {
-    Form form;
-    int split;
-};
-
-// rows16: rows of x and w start at multiples of 16 bytes and K is a multiple of 8.  odd: some row may not start at a multiple
-// of 4 bytes.
-Choice choose_form(const MatmulArgs &a, bool rows16, bool odd, int n_cu, size_t ws_bytes) {
-    Choice best{STAGED, 1};
-    double t = 1e30;
-    auto consider = [&](Form f, int split, double cost) {
-        if (cost < t) {
-            t = cost;
-            best = Choice{f, split};
-        }
-    };
-    if (!rows16) {
-        // odd rows: 787 x 333 x 1001 direct 9.8 us and staged 19.1, x 1002 8.0 and 13.5; 8192 x 2047 x 2047 staged 200 us,
-        // 8192 x 2048 x 2046 155
-        consider(DIRECT, 1, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
-        consider(DIRECT22, 1, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
-        consider(STAGED, 1, (odd ? 1.4 : 1.0) * tile_cost(kStaged, a, 1, n_cu));
-        return best;
-    }
-    // Forms that cannot be the fastest are not looked at: an estimate costs the host 30 ns.
-    const double tiles = 1.0 * ceil_div(a.M, 64) * ceil_div(a.N, 64);
-    if (tiles <= 3.0 * n_cu) {
-        consider(RING11, 1, ring_cost(kRing11, a, n_cu));
-        consider(RING11W, 1, ring_cost(kRing11W, a, n_cu));
-        consider(RING12, 1, ring_cost(kRing12, a, n_cu));
-        if (a.M > 16) {
-            consider(RING22, 1, ring_cost(kRing22, a, n_cu));
-            consider(RING42, 1, ring_cost(kRing42, a, n_cu));
-            consider(RING44, 1, ring_cost(kRing44, a, n_cu));
-        }
-    }
-    if (a.M > 16) consider(TILE64, 1, tile_cost(kTile64, a, 1, n_cu));
-    if (tiles >= n_cu) {
-        consider(TILE128x64, 1, tile_cost(kTile128x64, a, 1, n_cu));
-        consider(TILE128, 1, tile_cost(kTile128, a, 1, n_cu));
-    }
-    if (tiles >= 4.0 * n_cu) consider(BIG, 1, tile_cost(kBig, a, 1, n_cu));
-    const size_t plane = 4ull * a.M * a.N;
-    if (a.M <= 16 || tiles > 2.0 * n_cu || plane >= (1ull << 32)) return best;
-    for (int split = 2; split <= kMaxSplit && split * plane <= ws_bytes && split <= ceil_div(a.K, 64); split *= 2)
-        consider(TILE64, split, tile_cost(kTile64, a, split, n_cu));
-    return best;
+bool aligned(const void *q, int ld, int n) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % n == 0); }
+// Some row of x or w may not start at a multiple of 4 bytes.
+bool rows_odd(const MatmulArgs &a) {
+    return (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 4 != 0 || ((a.ldx | a.ldw) & 1) != 0;
 }
 
 template <int BM, int BN>
@@ -884,26 +839,26 @@ hipError_t launch_split(Params &p, hipStream_t stream) {
 }
 
 template <typename T, typename TO, ActCode A>
-hipError_t launch_act(Params &p, const Choice &c, bool odd, hipStream_t stream) {
+hipError_t launch_act(Params &p, const MatmulChoice &c, bool odd, hipStream_t stream) {
     if (p.splits > 1) return launch_split<T, TO, A>(p, stream);
     switch (c.form) {
-        case RING11: launch_ring<T, TO, A, 1, 1, 4, 4>(p, stream); break;
-        case RING11W: launch_ring<T, TO, A, 1, 1, 16, 2>(p, stream); break;
-        case RING12: launch_ring<T, TO, A, 1, 2, 8, 3>(p, stream); break;
-        case RING22: launch_ring<T, TO, A, 2, 2, 4, 2>(p, stream); break;
-        case RING42: launch_ring<T, TO, A, 4, 2, 4, 3>(p, stream); break;
-        case RING44: launch_ring<T, TO, A, 4, 4, 4, 2>(p, stream); break;
-        case DIRECT: launch_direct<T, TO, A, 1, 1, 8>(p, odd, stream); break;
-        case DIRECT22: launch_direct<T, TO, A, 2, 2, 8>(p, odd, stream); break;
-        case TILE64: launch_tile<T, TO, A, 64, 64>(p, stream); break;
-        case TILE128x64: launch_tile<T, TO, A, 128, 64>(p, stream); break;
-        case TILE128: launch_tile<T, TO, A, 128, 128>(p, stream); break;
-        case BIG: {
+        case MatmulForm::RING11: launch_ring<T, TO, A, 1, 1, 4, 4>(p, stream); break;
+        case MatmulForm::RING11W: launch_ring<T, TO, A, 1, 1, 16, 2>(p, stream); break;
+        case MatmulForm::RING12: launch_ring<T, TO, A, 1, 2, 8, 3>(p, stream); break;
+        case MatmulForm::RING22: launch_ring<T, TO, A, 2, 2, 4, 2>(p, stream); break;
+        case MatmulForm::RING42: launch_ring<T, TO, A, 4, 2, 4, 3>(p, stream); break;
+        case MatmulForm::RING44: launch_ring<T, TO, A, 4, 4, 4, 2>(p, stream); break;
+        case MatmulForm::DIRECT: launch_direct<T, TO, A, 1, 1, 8>(p, odd, stream); break;
+        case MatmulForm::DIRECT22: launch_direct<T, TO, A, 2, 2, 8>(p, odd, stream); break;
+        case MatmulForm::TILE64: launch_tile<T, TO, A, 64, 64>(p, stream); break;
+        case MatmulForm::TILE128x64: launch_tile<T, TO, A, 128, 64>(p, stream); break;
+        case MatmulForm::TILE128: launch_tile<T, TO, A, 128, 128>(p, stream); break;
+        case MatmulForm::BIG: {
             const dim3 grid = set_grid<256, 256>(p);
             big_tile_kernel<T, TO, A, 256, 2, 4><<<grid, 512, 0, stream>>>(p);
             break;
         }
-        case STAGED: {
+        case MatmulForm::STAGED: {
             set_grid<64, 64>(p);
             if (odd) staged_kernel<T, TO, A, true><<<dim3(p.total), 256, 0, stream>>>(p);
             else staged_kernel<T, TO, A, false><<<dim3(p.total), 256, 0, stream>>>(p);
@@ -914,7 +869,7 @@ hipError_t launch_act(Params &p, const Choice &c, bool odd, hipStream_t stream) 
 }
 
 template <typename T, typename TO>
-hipError_t launch_types(Params &p, const Choice &c, bool odd, hipStream_t stream) {
+hipError_t launch_types(Params &p, const MatmulChoice &c, bool odd, hipStream_t stream) {
     switch (act_code(p.act)) {
         case ActCode::NORMAL: return launch_act<T, TO, ActCode::NORMAL>(p, c, odd, stream);
         case ActCode::GATE: return launch_act<T, TO, ActCode::GATE>(p, c, odd, stream);
@@ -922,17 +877,56 @@ hipError_t launch_types(Params &p, const Choice &c, bool odd, hipStream_t stream
     }
 }
 
-bool aligned(const void *q, int ld, int n) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % n == 0); }
-bool rows_aligned(const MatmulArgs &a) { return aligned(a.x, a.ldx, 8) && aligned(a.w, a.ldw, 8) && a.K % 8 == 0; }
-bool rows_odd(const MatmulArgs &a) {
-    return (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 4 != 0 || ((a.ldx | a.ldw) & 1) != 0;
-}
-
 }  // namespace
+
+MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu) {
+    typedef MatmulForm F;
+    MatmulChoice best{F::STAGED, 1};
+    double t = 1e30;
+    auto consider = [&](F f, int split, double cost) {
+        if (cost < t) {
+            t = cost;
+            best = MatmulChoice{f, split};
+        }
+    };
+    // the transfers to LDS bring aligned 16 bytes
+    if (!(aligned(a.x, a.ldx, 8) && aligned(a.w, a.ldw, 8) && a.K % 8 == 0)) {
+        const bool odd = rows_odd(a);
+        // odd rows: 787 x 333 x 1001 direct 9.8 us and staged 19.1, x 1002 8.0 and 13.5; 8192 x 2047 x 2047 staged 200 us,
+        // 8192 x 2048 x 2046 155
+        consider(F::DIRECT, 1, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
+        consider(F::DIRECT22, 1, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
+        consider(F::STAGED, 1, (odd ? 1.4 : 1.0) * tile_cost(kStaged, a, 1, n_cu));
+        return best;
+    }
+    // Forms that cannot be the fastest are not looked at: an estimate costs the host 30 ns.
+    const double tiles = 1.0 * ceil_div(a.M, 64) * ceil_div(a.N, 64);
+    if (a.M <= 64 || tiles <= 3.0 * n_cu) {
+        consider(F::RING11, 1, ring_cost(kRing11, a, n_cu));
+        consider(F::RING11W, 1, ring_cost(kRing11W, a, n_cu));
+        consider(F::RING12, 1, ring_cost(kRing12, a, n_cu));
+        if (a.M > 16) {
+            consider(F::RING22, 1, ring_cost(kRing22, a, n_cu));
+            consider(F::RING42, 1, ring_cost(kRing42, a, n_cu));
+            consider(F::RING44, 1, ring_cost(kRing44, a, n_cu));
+        }
+    }
+    if (a.M > 16) consider(F::TILE64, 1, tile_cost(kTile64, a, 1, n_cu));
+    if (tiles >= n_cu) {
+        consider(F::TILE128x64, 1, tile_cost(kTile128x64, a, 1, n_cu));
+        consider(F::TILE128, 1, tile_cost(kTile128, a, 1, n_cu));
+    }
+    if (tiles >= 4.0 * n_cu) consider(F::BIG, 1, tile_cost(kBig, a, 1, n_cu));
+    const size_t plane = 4ull * a.M * a.N;
+    if (a.M <= 16 || tiles > 2.0 * n_cu || plane >= (1ull << 32)) return best;
+    for (int split = 2; split <= kMaxSplit && split * plane <= (a.ws ? a.ws_bytes : 0) && split <= ceil_div(a.K, 64); split *= 2)
+        consider(F::TILE64, split, tile_cost(kTile64, a, split, n_cu));
+    return best;
+}
 
 hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
     const bool odd = rows_odd(a);
-    const Choice c = choose_form(a, rows_aligned(a), odd, ctx.n_cu, a.ws ? a.ws_bytes : 0);
+    const MatmulChoice c = choose_matmul(a, ctx.n_cu);
     if (launches) *launches = c.split > 1 ? 2 : 1;
     Params p{};
     p.x = a.x; p.w = a.w; p.b = a.b; p.r = a.residual; p.y = a.y;
@@ -950,9 +944,11 @@ hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t 
 }
 
 size_t matmul_workspace(const MatmulArgs &a) {
+    MatmulArgs all = a;
+    all.ws = &all;   // any address: nothing is launched
+    all.ws_bytes = ~static_cast<size_t>(0);
     int split = 1;
-    for (int n_cu = 32; n_cu <= 256; n_cu += 32)
-        split = std::max(split, choose_form(a, rows_aligned(a), rows_odd(a), n_cu, ~static_cast<size_t>(0)).split);
+    for (int n_cu = 32; n_cu <= 256; n_cu += 32) split = std::max(split, choose_matmul(all, n_cu).split);
     return split == 1 ? 0 : (4ull * split * a.M * a.N + 255) / 256 * 256;
 }
 

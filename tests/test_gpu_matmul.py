@@ -86,7 +86,9 @@ class Case:
 SIZES = [(1, 1, 1), (1, 1, 8), (1, 64, 64), (2, 3, 5), (1, 1000, 2048), (1, 33, 4096), (3, 17, 1000), (4, 512, 72), (5, 128, 8200),
          (8, 100, 520), (16, 16, 32), (17, 40, 96), (24, 1024, 512), (31, 65, 127), (33, 257, 264), (48, 96, 4104), (63, 64, 65),
          (64, 64, 64), (65, 63, 1), (100, 300, 2056), (128, 128, 128), (129, 136, 200), (197, 320, 640), (255, 257, 33), (256, 256, 64),
-         (257, 512, 72), (300, 8, 1024), (520, 264, 96), (1000, 24, 40), (1024, 768, 256), (777, 1031, 129)]
+         (257, 512, 72), (300, 8, 1024), (520, 264, 96), (1000, 24, 40), (1024, 768, 256), (777, 1031, 129),
+         (9, 1000, 3000), (2, 16400, 64), (60, 1100, 1288), (1300, 200, 4096), (2156, 2560, 72), (2049, 1032, 328), (2560, 2310, 712), (16, 4104, 40),
+         (523, 1264, 2552), (4100, 4104, 520)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
@@ -95,10 +97,10 @@ def test_integers_are_exact(size):
     M, N, K = size
     for dtype, out in (("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16")):
         c = Case(1, M, N, K, dtype, out, res=True, integers=True)
-        want = (c.x.double().cpu() @ c.w.double().cpu().t() + c.b.double().cpu() + c.r.double().cpu()).to(c.out[0])
+        want = (c.x.double() @ c.w.double().t().contiguous() + c.b.double() + c.r.double()).to(c.out[0])
         for workspace in (True, False):
             c.y.fill_(GUARD)
-            assert torch.equal(c.run(workspace=workspace).cpu(), want), (dtype, out, workspace)
+            assert torch.equal(c.run(workspace=workspace), want), (dtype, out, workspace)
             c.check_guards()
 
 
