@@ -508,16 +508,17 @@ typedef struct gpulet_matmul_desc {
     int32_t dtype, out_dtype, act;
 } gpulet_matmul_desc;
 
-/* Bytes of workspace with which gpulet_matmul is fastest on any number of CUs (0
- * for most shapes: it is for few rows and a long K, whose depth is split over
- * workgroups).  Needs no GPU.  Errors as gpulet_matmul. */
+/* Bytes of workspace with which gpulet_matmul is fastest on any number of CUs: 0
+ * for most shapes; partial sums where few tiles have a long K, and copies of x or
+ * w where a large product's rows do not start at multiples of 16 bytes.  Needs no
+ * GPU.  Errors as gpulet_matmul. */
 gpulet_status gpulet_matmul_workspace_bytes(const gpulet_matmul_desc *d, size_t *bytes);
 
 /* Enqueues the product on `stream`.  `workspace` is device memory of
  * workspace_bytes bytes that nothing else uses until the work is done (calls on
  * one stream may share it, graphs that may run at the same time may not); what it
  * holds before does not matter.  NULL or fewer bytes than asked for are allowed:
- * the depth is then split less or not at all. */
+ * the product then runs without what does not fit. */
 gpulet_status gpulet_matmul(const gpulet_matmul_desc *d, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

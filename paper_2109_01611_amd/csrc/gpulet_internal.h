@@ -147,11 +147,13 @@ struct MatmulArgs {
     void *ws;
     size_t ws_bytes;
 };
-// The form a product runs in on n_cu CUs (matmul.hip) and how many workgroups share the depth of a tile, given a.ws.
+// The form a product runs in on n_cu CUs (matmul.hip), how many workgroups share the depth of a tile, and whether operands
+// whose rows do not start at multiples of 16 bytes are laid out anew first, given a.ws.
 enum class MatmulForm { RING11, RING11W, RING12, RING22, RING42, RING44, TILE64, TILE128x64, TILE128, BIG, DIRECT, DIRECT22, STAGED };
 struct MatmulChoice {
     MatmulForm form;
     int split;
+    bool pack;
 };
 MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu);
 gpulet_status check_matmul(const gpulet_matmul_desc *d, MatmulArgs &a);

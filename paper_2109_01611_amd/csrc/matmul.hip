@@ -10,12 +10,13 @@
 //   tile     64x64, 128x64 and 128x128 tiles that a workgroup goes through slice by slice.  Bound by the rate at which a CU
 //            takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128 56 us, 933 TFLOP/s.
 //            The 64x64 one also with a depth that up to eight workgroups share, whose sums meet in the workspace: tall y with
-//            few tiles and a long depth (5470 x 88 x 2504 15.9 us, in rings 18.4).
+//            few tiles and a long depth (1742 x 216 x 3816 16.3 us, in rings 20.4).
 //   big      256x256 tiles, 160 KB of LDS: as many matrix instructions as transfers can feed.  8192 x 4096 x 4096 216 us,
 //            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 1.33.
 //   direct,  rows that do not start at multiples of 16 bytes or a depth that is not a multiple of 8: operands go from memory
 //   staged   into the matrix instructions (few rows, few tiles), or through registers into LDS (64x64 tiles).
-//            2048 x 1024 x 1001 19 us.
+//            200 x 300 x 4001 9.6 us.  Larger products of such operands lay them out anew in the workspace first and
+//            take the forms above: 2048 x 1024 x 1001 18.5 us (staged 23.2), 4096 x 4096 x 1022 50.5 (88.1).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -52,31 +53,25 @@ struct Params {
     int slices;             // slices of the depth: of 64, a workgroup's (splits > 1) or a wavefront's (ring); of 32, a
                             // wavefront's (direct)
     float *part;            // splits > 1: [split][M][N] sums
-    int vec;                // rows of y and the residual allow 16-byte accesses
     FastDiv d_tiles, d_tiles_n, d_tiles_m;
 };
 
-template <int N> struct Bytes;
-template <> struct Bytes<8> { typedef uint2 Type; };
-template <> struct Bytes<16> { typedef uint4 Type; };
-
-// bias, residual and activation on NC consecutive columns of row m, then the store; `full`: all of them exist and can be
-// reached 16 bytes at a time.  `bias` holds the columns' bias.
+// bias, residual and activation on NC consecutive columns of row m, then the store; `bias` holds the columns' bias.  Rows of y
+// and the residual may start anywhere: 16 bytes at a time they cost less than element by element at any alignment (12965 x
+// 3053 x 280 fp16 153 us element by element).
 template <int NC, typename T, ActCode A>
-__device__ __forceinline__ void finish(const Params &p, int m, int n, bool full, const float (&bias)[NC], float (&v)[NC]) {
+__device__ __forceinline__ void finish(const Params &p, int m, int n, const float (&bias)[NC], float (&v)[NC]) {
     const T *r = p.r ? static_cast<const T *>(p.r) + static_cast<long long>(m) * p.ldr + n : nullptr;
     T *y = static_cast<T *>(p.y) + static_cast<long long>(m) * p.ldy + n;
-    typedef typename Bytes<NC * sizeof(T) < 16 ? 8 : 16>::Type Raw;
-    constexpr int PER = sizeof(Raw) / sizeof(T);   // elements of an access
+    constexpr int PER = NC * sizeof(T) < 16 ? NC : 16 / sizeof(T);   // elements of an access
 #pragma unroll
     for (int i = 0; i < NC; ++i) v[i] += bias[i];
-    if (NC % PER == 0 && full) {
+    if (n + NC <= p.N) {
+        T e[PER];
         if (r) {
 #pragma unroll
             for (int i = 0; i < NC; i += PER) {
-                T e[PER];
-                const Raw u = *reinterpret_cast<const Raw *>(r + i);
-                __builtin_memcpy(e, &u, sizeof(u));
+                __builtin_memcpy(e, r + i, sizeof(e));
 #pragma unroll
                 for (int j = 0; j < PER; ++j) v[i + j] += static_cast<float>(e[j]);
             }
@@ -84,12 +79,9 @@ __device__ __forceinline__ void finish(const Params &p, int m, int n, bool full,
         activate<A>(v, p.act);
 #pragma unroll
         for (int i = 0; i < NC; i += PER) {
-            T e[PER];
 #pragma unroll
             for (int j = 0; j < PER; ++j) e[j] = static_cast<T>(v[i + j]);
-            Raw u;
-            __builtin_memcpy(&u, e, sizeof(u));
-            *reinterpret_cast<Raw *>(y + i) = u;
+            __builtin_memcpy(y + i, e, sizeof(e));
         }
         return;
     }
@@ -233,7 +225,7 @@ __global__ __launch_bounds__(256) void staged_kernel(Params p) {
         for (int i = 0; i < 2; ++i) {
             const int m = m0 + wm + 16 * i + (lane & 15);
             float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (m < p.M && n < p.N) finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
+            if (m < p.M && n < p.N) finish<4, TO, A>(p, m, n, bias, v);
         }
     }
 }
@@ -367,7 +359,6 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Params p) {
     const int n = n0 + wn * (BN / WN) + (lane >> 4) * NC;
     float bias[NC];
     if (!SPLIT) load_bias(p, n, bias);
-    const bool full = p.vec && n + NC <= p.N;
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
         const int m = m0 + wm * (BM / WM) + 16 * i + fr;
@@ -386,7 +377,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Params p) {
                     if (n + j < p.N) y[j] = v[j];
             }
         } else {
-            finish<NC, TO, A>(p, m, n, full, bias, v);
+            finish<NC, TO, A>(p, m, n, bias, v);
         }
     }
 }
@@ -498,7 +489,6 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
     const int n = n0 + wn * (BN / WN) + (lane >> 4) * NC;
     float bias[NC];
     load_bias(p, n, bias);
-    const bool full = p.vec && n + NC <= p.N;
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
         const int m = m0 + wm * (BM / WM) + 16 * i + fr;
@@ -506,7 +496,7 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
         float v[NC];
 #pragma unroll
         for (int j = 0; j < NC; ++j) v[j] = acc[i][j >> 2][j & 3];
-        finish<NC, TO, A>(p, m, n, full, bias, v);
+        finish<NC, TO, A>(p, m, n, bias, v);
     }
 }
 
@@ -612,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
         if (m >= p.M || n >= p.N) continue;
         float v[4] = {s[0], s[1], s[2], s[3]}, bias[4];
         load_bias(p, n, bias);
-        finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
+        finish<4, TO, A>(p, m, n, bias, v);
     }
 }
 
@@ -702,8 +692,41 @@ __global__ __launch_bounds__(64 * WAVES) void ring_kernel(Params p) {
         if (m >= p.M || n >= p.N) continue;
         float v[4] = {s[0], s[1], s[2], s[3]}, bias[4];
         load_bias(p, n, bias);
-        finish<4, TO, A>(p, m, n, p.vec && n + 4 <= p.N, bias, v);
+        finish<4, TO, A>(p, m, n, bias, v);
     }
+}
+
+// ---- rows laid out anew
+
+// Rows of K elements that start anywhere -> rows of Kp, a multiple of 8, that start at multiples of 16 bytes, with zeros behind
+// the last element; up to two operands.
+struct Pack {
+    const void *src[2];
+    void *dst[2];
+    int ld[2];
+    int K, Kp;
+    int first, items;      // chunks of 8 elements of the first operand and of both
+    FastDiv d_chunks;      // by Kp / 8
+};
+// A thread brings 8 elements; the dword behind unaligned ones comes from its neighbour, as above.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(Pack p) {
+    const int i = blockIdx.x * 256 + threadIdx.x, which = i >= p.first, j = i - (which ? p.first : 0);
+    const int row = fdiv(j, p.d_chunks), k = (j - row * (p.Kp / 8)) * 8, lane = threadIdx.x & 63;
+    const bool in = i < p.items;
+    const T *r = static_cast<const T *>(p.src[which]) + (in ? static_cast<long long>(row) * p.ld[which] : 0);
+    const bool whole = in && k + 8 <= p.K, last = lane == 63 || k + 16 > p.K;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    unsigned tail = 0;
+    if (whole) {
+        v = load_floor(r + k);
+        if (last) tail = load_tail(r + k);
+    }
+    unsigned behind = __shfl_down(v.x, 1);
+    if (last) behind = tail;
+    if (whole) v = shift_in(v, behind, r + k);
+    else if (in) v = load_cut(r, k, p.K);
+    if (in) *reinterpret_cast<uint4 *>(static_cast<T *>(p.dst[which]) + static_cast<long long>(row) * p.Kp + k) = v;
 }
 
 // ---- a depth that several workgroups share
@@ -729,7 +752,7 @@ __global__ __launch_bounds__(256) void join_kernel(Params p) {
             for (int j = 0; j < 4; ++j)
                 if (n + j < p.N) v[j] += p.part[k * plane + at + j];
     }
-    finish<4, TO, A>(p, static_cast<int>(m), n, p.vec && n + 4 <= p.N, bias, v);
+    finish<4, TO, A>(p, static_cast<int>(m), n, bias, v);
 }
 
 // ---- host side
@@ -747,19 +770,23 @@ constexpr TileCost kTile64 = {64, 64, 5, 0.5, 0.0, 0.46, 0.25, 0.45}, kTile128x6
                    kTile128 = {128, 128, 2, 0.0, 0.44, 0.29, 0.44, 3.2}, kBig = {256, 256, 1, 4.0, 1.35, 0.1, 1.45, 6.0},
                    kStaged = {64, 64, 5, 0.5, 0.50, 0.10, 0.29, 0.46};
 // The wavefronts of a ring or direct form work side by side on slices of 64; a round takes as long as its slices one after the
-// other or as its operands at `per_kb`.
+// other or as its operands at `per_kb`, and a workgroup of a direct form no less than `least`.
 struct RingCost {
     int mb, nb, waves, resident;
-    double round, near, far, per_kb, finish;
+    double round, near, far, per_kb, finish, least;
 };
-constexpr RingCost kRing11 = {1, 1, 4, 2, 0.1, 0.17, 0.06, 0.0142, 0.36}, kRing11W = {1, 1, 16, 1, 0.45, 0.16, 0.60, 0.0072, 0.44},
-                   kRing12 = {1, 2, 8, 1, 0.32, 0.10, 0.63, 0.0079, 0.61}, kRing22 = {2, 2, 4, 2, 0.0, 0.27, 0.09, 0.014, 0.68},
-                   kRing42 = {4, 2, 4, 1, 0.07, 0.37, 0.09, 0.0175, 1.15}, kRing44 = {4, 4, 4, 1, 1.8, 0.06, 0.56, 0.0172, 0.35},
-                   kDirect = {1, 1, 8, 4, 0.2, 0.31, 0.0, 0.021, 0.0}, kDirect22 = {2, 2, 8, 2, 0.0, 0.73, 0.0, 0.027, 0.0};
+constexpr RingCost kRing11 = {1, 1, 4, 2, 0.1, 0.17, 0.06, 0.0142, 0.36, 0.0}, kRing11W = {1, 1, 16, 1, 0.45, 0.16, 0.60, 0.0072, 0.44, 0.0},
+                   kRing12 = {1, 2, 8, 1, 0.32, 0.10, 0.63, 0.0079, 0.61, 0.0}, kRing22 = {2, 2, 4, 2, 0.0, 0.27, 0.09, 0.014, 0.68, 0.0},
+                   kRing42 = {4, 2, 4, 1, 0.07, 0.37, 0.09, 0.0175, 1.15, 0.0}, kRing44 = {4, 4, 4, 1, 1.8, 0.06, 0.56, 0.0172, 0.35, 0.0},
+                   kDirect = {1, 1, 8, 4, 0.2, 0.31, 0.0, 0.021, 0.0, 0.65}, kDirect22 = {2, 2, 8, 2, 0.0, 0.73, 0.0, 0.027, 0.0, 1.3};
 constexpr double kStart = 2.2;
-// The launch that joins a shared depth: itself and what the host needs for it, and its traffic by the megabyte.
-constexpr double kJoin = 4.9, kJoinMb = 0.34;
+// The launch that joins a shared depth, and its traffic by the megabyte.
+constexpr double kJoin = 2.5, kJoinMb = 0.34;
 constexpr int kMaxSplit = 8;
+// The launch that lays rows out anew, likewise.
+constexpr double kPack = 4.5, kPackMb = 0.3;
+// What a call of more than one launch takes the host, and each launch of it: a shorter call waits for the host.
+constexpr double kCall = 3.5, kLaunch = 3.2;
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -772,7 +799,7 @@ double tile_cost(const TileCost &c, const MatmulArgs &a, int split, int n_cu) {
     auto round = [&](int wgs) { return c.round + slices * std::max(alone, c.busy * wgs); };
     const int rest = n % c.resident;
     double t = kStart + n / c.resident * round(c.resident) + (rest ? round(rest) : 0.0) + c.finish * n;
-    if (split > 1) t += kJoin + kJoinMb * 4e-6 * split * a.M * a.N;
+    if (split > 1) t = std::max(t + kJoin + kJoinMb * 4e-6 * split * a.M * a.N, kCall + 2 * kLaunch);
     return t;
 }
 
@@ -782,10 +809,17 @@ double ring_cost(const RingCost &c, const MatmulArgs &a, int n_cu, double slower
     const int n = static_cast<int>((wgs + n_cu - 1) / n_cu), rounds = ceil_div(n, c.resident);
     const double kb = (std::min(a.M, 16 * c.mb) + std::min(a.N, 16 * c.nb)) * (a.K * 2.0 / 1024);
     const double chain = 1.0 * rounds * ceil_div(ceil_div(a.K, 64), c.waves) * (c.near + c.far * from_memory(a));
-    return kStart + rounds * c.round + slower * std::max(chain, n * kb * c.per_kb) + c.finish * n;
+    return kStart + rounds * c.round + slower * std::max(std::max(chain, n * c.least), n * kb * c.per_kb) + c.finish * n;
 }
 
-bool aligned(const void *q, int ld, int n) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % n == 0); }
+int padded(int K) { return (K + 7) / 8 * 8; }
+// The transfers to LDS bring aligned 16 bytes.
+bool x_aligned(const MatmulArgs &a) { return reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx % 8 == 0 && a.K % 8 == 0; }
+bool w_aligned(const MatmulArgs &a) { return reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && a.ldw % 8 == 0 && a.K % 8 == 0; }
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t pack_x_bytes(const MatmulArgs &a) { return x_aligned(a) ? 0 : round256(2ull * a.M * padded(a.K)); }
+size_t pack_w_bytes(const MatmulArgs &a) { return w_aligned(a) ? 0 : round256(2ull * a.N * padded(a.K)); }
+size_t pack_bytes(const MatmulArgs &a) { return pack_x_bytes(a) + pack_w_bytes(a); }
 // Some row of x or w may not start at a multiple of 4 bytes.
 bool rows_odd(const MatmulArgs &a) {
     return (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 4 != 0 || ((a.ldx | a.ldw) & 1) != 0;
@@ -877,28 +911,16 @@ hipError_t launch_types(Params &p, const MatmulChoice &c, bool odd, hipStream_t 
     }
 }
 
-}  // namespace
-
-MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu) {
+// The form for rows that start at multiples of 16 bytes, and its time.
+double choose_aligned(const MatmulArgs &a, int n_cu, size_t ws_bytes, MatmulChoice &best) {
     typedef MatmulForm F;
-    MatmulChoice best{F::STAGED, 1};
     double t = 1e30;
     auto consider = [&](F f, int split, double cost) {
         if (cost < t) {
             t = cost;
-            best = MatmulChoice{f, split};
+            best = MatmulChoice{f, split, false};
         }
     };
-    // the transfers to LDS bring aligned 16 bytes
-    if (!(aligned(a.x, a.ldx, 8) && aligned(a.w, a.ldw, 8) && a.K % 8 == 0)) {
-        const bool odd = rows_odd(a);
-        // odd rows: 787 x 333 x 1001 direct 9.8 us and staged 19.1, x 1002 8.0 and 13.5; 8192 x 2047 x 2047 staged 200 us,
-        // 8192 x 2048 x 2046 155
-        consider(F::DIRECT, 1, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
-        consider(F::DIRECT22, 1, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
-        consider(F::STAGED, 1, (odd ? 1.4 : 1.0) * tile_cost(kStaged, a, 1, n_cu));
-        return best;
-    }
     // Forms that cannot be the fastest are not looked at: an estimate costs the host 30 ns.
     const double tiles = 1.0 * ceil_div(a.M, 64) * ceil_div(a.N, 64);
     if (a.M <= 64 || tiles <= 3.0 * n_cu) {
@@ -918,25 +940,85 @@ MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu) {
     }
     if (tiles >= 4.0 * n_cu) consider(F::BIG, 1, tile_cost(kBig, a, 1, n_cu));
     const size_t plane = 4ull * a.M * a.N;
-    if (a.M <= 16 || tiles > 2.0 * n_cu || plane >= (1ull << 32)) return best;
-    for (int split = 2; split <= kMaxSplit && split * plane <= (a.ws ? a.ws_bytes : 0) && split <= ceil_div(a.K, 64); split *= 2)
+    if (a.M <= 16 || tiles > 2.0 * n_cu || plane >= (1ull << 32)) return t;
+    for (int split = 2; split <= kMaxSplit && split * plane <= ws_bytes && split <= ceil_div(a.K, 64); split *= 2)
         consider(F::TILE64, split, tile_cost(kTile64, a, split, n_cu));
+    return t;
+}
+
+}  // namespace
+
+MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu) {
+    const size_t ws_bytes = a.ws ? a.ws_bytes : 0;
+    MatmulChoice best{MatmulForm::STAGED, 1, false};
+    if (x_aligned(a) && w_aligned(a)) {
+        choose_aligned(a, n_cu, ws_bytes, best);
+        return best;
+    }
+    // odd rows: 787 x 333 x 1001 direct 9.8 us and staged 19.1, x 1002 8.0 and 13.5; 8192 x 2047 x 2047 staged 200 us,
+    // 8192 x 2048 x 2046 155
+    const bool odd = rows_odd(a);
+    double t = (odd ? 1.4 : 1.0) * tile_cost(kStaged, a, 1, n_cu);
+    auto consider = [&](const MatmulChoice &c, double cost) {
+        if (cost < t) {
+            t = cost;
+            best = c;
+        }
+    };
+    consider({MatmulForm::DIRECT, 1, false}, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
+    consider({MatmulForm::DIRECT22, 1, false}, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
+    const size_t room = pack_bytes(a);
+    if (t > kPack && room <= ws_bytes && room < (1ull << 34)) {   // chunks are counted below 2^30
+        MatmulArgs b = a;
+        b.K = padded(a.K);
+        MatmulChoice c{};
+        const double cost = kPack + kPackMb * 1e-6 * room + choose_aligned(b, n_cu, ws_bytes - room, c);
+        c.pack = true;
+        consider(c, std::max(cost, kCall + (c.split > 1 ? 3 : 2) * kLaunch));
+    }
     return best;
 }
 
-hipError_t launch_matmul(const MatmulArgs &a, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
-    const bool odd = rows_odd(a);
+hipError_t launch_matmul(const MatmulArgs &args, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
+    MatmulArgs a = args;
     const MatmulChoice c = choose_matmul(a, ctx.n_cu);
-    if (launches) *launches = c.split > 1 ? 2 : 1;
+    if (launches) *launches = (c.pack ? 1 : 0) + (c.split > 1 ? 2 : 1);
+    char *ws = static_cast<char *>(a.ws);
+    if (c.pack) {
+        Pack k{};
+        k.K = a.K;
+        k.Kp = padded(a.K);
+        const int chunks = k.Kp / 8;
+        k.d_chunks = make_fastdiv(chunks);
+        auto add = [&](const void *src, int ld, int rows, size_t bytes) -> const void * {
+            if (bytes == 0) return src;
+            const int at = k.items == 0 ? 0 : 1;
+            k.src[at] = src; k.dst[at] = ws; k.ld[at] = ld;
+            k.items += rows * chunks;
+            if (at == 0) k.first = k.items;
+            ws += bytes;
+            return k.dst[at];
+        };
+        const size_t xb = pack_x_bytes(a), wb = pack_w_bytes(a);
+        a.x = add(a.x, a.ldx, a.M, xb);
+        a.w = add(a.w, a.ldw, a.N, wb);
+        if (xb) a.ldx = k.Kp;
+        if (wb) a.ldw = k.Kp;
+        a.K = k.Kp;
+        const dim3 grid((static_cast<unsigned>(k.items) + 255) / 256);
+        if (a.dtype == GPULET_BF16) pack_kernel<__bf16><<<grid, 256, 0, stream>>>(k);
+        else pack_kernel<_Float16><<<grid, 256, 0, stream>>>(k);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const bool odd = rows_odd(a);
     Params p{};
     p.x = a.x; p.w = a.w; p.b = a.b; p.r = a.residual; p.y = a.y;
     p.M = a.M; p.N = a.N; p.K = a.K;
     p.ldx = a.ldx; p.ldw = a.ldw; p.ldr = a.ldr; p.ldy = a.ldy;
     p.act = a.act;
     p.splits = c.split;
-    p.part = static_cast<float *>(a.ws);
-    const int per = a.out_dtype == GPULET_F32 ? 4 : 8;
-    p.vec = aligned(a.y, a.ldy, per) && aligned(a.residual, a.ldr, per);
+    p.part = reinterpret_cast<float *>(ws);
     if (a.dtype == GPULET_BF16)
         return a.out_dtype == GPULET_F32 ? launch_types<__bf16, float>(p, c, odd, stream) : launch_types<__bf16, __bf16>(p, c, odd, stream);
     return a.out_dtype == GPULET_F32 ? launch_types<_Float16, float>(p, c, odd, stream)
@@ -947,9 +1029,12 @@ size_t matmul_workspace(const MatmulArgs &a) {
     MatmulArgs all = a;
     all.ws = &all;   // any address: nothing is launched
     all.ws_bytes = ~static_cast<size_t>(0);
-    int split = 1;
-    for (int n_cu = 32; n_cu <= 256; n_cu += 32) split = std::max(split, choose_matmul(all, n_cu).split);
-    return split == 1 ? 0 : (4ull * split * a.M * a.N + 255) / 256 * 256;
+    size_t bytes = 0;
+    for (int n_cu = 32; n_cu <= 256; n_cu += 32) {
+        const MatmulChoice c = choose_matmul(all, n_cu);
+        bytes = std::max(bytes, (c.pack ? pack_bytes(a) : 0) + (c.split > 1 ? round256(4ull * c.split * a.M * a.N) : 0));
+    }
+    return bytes;
 }
 
 }  // namespace gpulet

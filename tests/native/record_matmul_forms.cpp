@@ -1,5 +1,5 @@
 // Prints the form the library would run a matrix product in.  Reads lines "n_cu M N K ldx shift workspace": shift in elements
-// from an aligned address, workspace in bytes.  Prints "form split".  No device is touched; the pointers are made up.
+// from an aligned address, workspace in bytes.  Prints "form split pack".  No device is touched; the pointers are made up.
 #include <cstdio>
 
 #include "gpulet_internal.h"
@@ -19,7 +19,7 @@ int main() {
         a.ws = ws ? reinterpret_cast<void *>(1ull << 53) : nullptr;
         a.ws_bytes = ws;
         const MatmulChoice c = choose_matmul(a, n_cu);
-        std::printf("%d %d\n", static_cast<int>(c.form), c.split);
+        std::printf("%d %d %d\n", static_cast<int>(c.form), c.split, c.pack);
     }
     return 0;
 }
