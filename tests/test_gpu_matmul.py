@@ -88,7 +88,7 @@ SIZES = [(1, 1, 1), (1, 1, 8), (1, 64, 64), (2, 3, 5), (1, 1000, 2048), (1, 33, 
          (64, 64, 64), (65, 63, 1), (100, 300, 2056), (128, 128, 128), (129, 136, 200), (197, 320, 640), (255, 257, 33), (256, 256, 64),
          (257, 512, 72), (300, 8, 1024), (520, 264, 96), (1000, 24, 40), (1024, 768, 256), (777, 1031, 129),
          (9, 1000, 3000), (2, 16400, 64), (60, 1100, 1288), (1300, 200, 4096), (2156, 2560, 72), (2049, 1032, 328), (2560, 2310, 712), (16, 4104, 40),
-         (523, 1264, 2552), (4100, 4104, 520), (4090, 4088, 520), (3240, 472, 897), (2300, 640, 1002), (3300, 4095, 517), (700, 600, 2001), (1742, 216, 3816), (1742, 217, 3815)]
+         (523, 1264, 2552), (4100, 4104, 520), (4090, 4088, 520), (3240, 472, 897), (2300, 640, 1002), (3300, 4095, 517), (700, 600, 2001), (1742, 216, 3816), (1742, 217, 3815), (8200, 4096, 72)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
