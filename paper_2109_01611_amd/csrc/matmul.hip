@@ -362,11 +362,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Params p) {
 
     // piece j of this wavefront: LDS rows 8 (wave + WAVES j) on; x rows first, then w rows
     unsigned voff[PIECES];
-    const int q = lane & 7;
+    static_assert(WAVES % 2 == 0, "pieces of a wavefront are whole 16 rows apart");
+    const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
         const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
-        const int chunk = q ^ ((row >> 1) & 7);
         if (j < XP) {
             voff[j] = row < mrows ? static_cast<unsigned>(row * p.ldx + chunk * 8) * 2u : OOB;
         } else {
@@ -382,10 +382,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Params p) {
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
             unsigned v = voff[j];
-            if (cut) {
-                const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
-                if (k + 8 * (q ^ ((row >> 1) & 7)) >= p.K) v = OOB;
-            }
+            if (cut && k + 8 * chunk >= p.K) v = OOB;
             dma16(j < XP ? xs : ws, to + (j < XP ? j * WAVES : BM / 8 + (j - XP) * WAVES) * 1024, v, k * 2);
         }
     };
@@ -465,11 +462,11 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
 
     // piece j of this wavefront: LDS rows 8 (wave + WAVES j) on; x rows first, then w rows
     unsigned voff[PIECES];
-    const int q = lane & 7;
+    static_assert(WAVES % 2 == 0, "pieces of a wavefront are whole 16 rows apart");
+    const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
         const int row = 8 * (wave + WAVES * (j < XP ? j : j - XP)) + (lane >> 3);
-        const int chunk = q ^ ((row >> 1) & 7);
         if (j < XP) {
             voff[j] = row < mrows ? static_cast<unsigned>(row * p.ldx + chunk * 8) * 2u : OOB;
         } else {
@@ -481,10 +478,7 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
     auto piece = [&](bool w, int j, int s, int slot) {
         const int k = s * 64;
         unsigned v = voff[j + (w ? XP : 0)];
-        if (k + 64 > p.K) {   // the last slice may be short: its missing chunks are zeros
-            const int row = 8 * (wave + WAVES * j) + (lane >> 3);
-            if (k + 8 * (q ^ ((row >> 1) & 7)) >= p.K) v = OOB;
-        }
+        if (k + 64 > p.K && k + 8 * chunk >= p.K) v = OOB;   // the last slice may be short: its missing chunks are zeros
         dma16(w ? ws : xs, base + slot * BM * 128 + wave * 1024 + j * WAVES * 1024, v, k * 2);
     };
     auto fetch = [&](bool w, int s, int slot) {
@@ -519,10 +513,10 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
         }
     };
 #pragma unroll
-    for (int i = 0; i < NBUF; ++i)
+    for (int i = 0; i < 4; ++i)
         if (i / 2 < n_slices) fetch(i & 1, i / 2, i);
     uint4 a0[NB], b0[MB], a1[NB], b1[MB];
-    if (n_slices >= 3) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(XP * 3) : "memory");
+    if (n_slices >= 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(XP * 2) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     read(a0, b0, 0, 1, c0);
     int at = 0;   // slot of x of slice s; w's is the next one
@@ -531,7 +525,7 @@ __global__ __launch_bounds__(64 * WM * WN) void big_tile_kernel(Params p) {
         const int wat = wrap(at + 1);
         read(a1, b1, at, wat, c1);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(a0, b0, s > 0 && s + 2 < n_slices, false, s + 2, wrap(at + NBUF - 1));
+        multiply(a0, b0, s + 2 < n_slices, false, s + 2, wrap(at + NBUF - 1));
         const int next = wrap(at + 2);
         if (s + 1 < n_slices) {
             // every wavefront has read all of slice s, and slice s + 1 is there; x of slice s + 2 may be on its way
@@ -1112,7 +1106,7 @@ size_t matmul_workspace(const MatmulArgs &a) {
     all.ws = &all;   // any address: nothing is launched
     all.ws_bytes = ~static_cast<size_t>(0);
     size_t bytes = 0;
-    for (int n_cu = 32; n_cu <= 256; n_cu += 32) {
+    for (int n_cu = 8; n_cu <= 256; n_cu += 8) {
         const MatmulChoice c = choose_matmul(all, n_cu);
         bytes = std::max(bytes, (c.pack ? pack_bytes(a) : 0) + (c.split > 1 ? round256(4ull * c.split * a.M * a.N) : 0));
     }
