@@ -237,3 +237,66 @@ def test_gpu_lets_and_graphs():
             c.run()
             assert not torch.equal(c.y, want)
             c.x.mul_(-1)
+
+
+PACKED = [(2500, 1000, 1032), (1500, 640, 1001)]
+
+
+@pytest.mark.parametrize("size", PACKED, ids=str)
+@pytest.mark.parametrize("pad", [(0, 0, 0, 0), (1, 0, 0, 0), (0, 3, 0, 0), (3, 5, 2, 9), (64, 24, 0, 0)], ids=str)
+def test_rows_laid_out_anew(size, pad):
+    # what lies between the rows and behind them is NaN: none of it may reach a sum
+    for shift in (1, 4):
+        c = Case(20, *size, dtype="bf16", out="bf16", act="gelu", res=True, pad=pad, shift=shift)
+        d = c.desc()
+        size_ = gpulet.matmul_workspace_bytes(d)
+        assert size_ > 0 or shift == 4
+        for view, flat in ((c.x, c.xf), (c.w, c.wf)):
+            kept = view.clone()
+            flat.fill_(float("nan"))
+            view.copy_(kept)
+        c.run()
+        c.check((pad, shift))
+        once = c.y.clone()
+        c.y.fill_(GUARD)
+        c.run(workspace=False)
+        c.check("without workspace")
+        for short in (256, size_ // 2 // 256 * 256, size_ - 256) if size_ else ():   # some of it
+            c.y.fill_(GUARD)
+            torch.cuda.synchronize()
+            gpulet.matmul(d, _workspace(size_), short)
+            torch.cuda.synchronize()
+            c.check(short)
+        c.y.fill_(GUARD)
+        assert torch.equal(c.run(), once)
+
+
+def test_rows_laid_out_anew_in_graphs_and_on_two_streams():
+    cs = [Case(30 + i, *size, res=True, act="silu", shift=1) for i, size in enumerate(PACKED)]
+    want = [c.run().clone() for c in cs]
+    descs = [c.desc() for c in cs]
+    sizes = [gpulet.matmul_workspace_bytes(d) for d in descs]
+    spaces = [_workspace(s) for s in sizes]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for d, ws, s in zip(descs, spaces, sizes):
+            gpulet.matmul(d, ws, s, torch.cuda.current_stream().cuda_stream)
+    for i in range(4):
+        for c in cs:
+            c.y.fill_(GUARD)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.y, w) for c, w in zip(cs, want))
+        for c in cs:
+            c.x.mul_(-1)
+            c.run()
+            c.x.mul_(-1)
+    streams = [torch.cuda.Stream() for _ in cs]
+    for c in cs:
+        c.y.fill_(GUARD)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, d, ws, s in zip(streams, descs, spaces, sizes):
+            gpulet.matmul(d, ws, s, st.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(c.y, w) for c, w in zip(cs, want))
