@@ -193,6 +193,14 @@ __device__ __forceinline__ uint4 shift_in(const uint4 &v, unsigned behind, const
     return make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, shift), __builtin_amdgcn_alignbit(v.z, v.y, shift),
                       __builtin_amdgcn_alignbit(v.w, v.z, shift), __builtin_amdgcn_alignbit(behind, v.w, shift));
 }
+// Elements s on (0 to 8) of eight, and zeros behind them.
+__device__ __forceinline__ uint4 drop(uint4 v, int s) {
+    if (s & 1) v = make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                              __builtin_amdgcn_alignbit(v.w, v.z, 16), v.w >> 16);
+    if (s & 2) v = make_uint4(v.y, v.z, v.w, 0u);
+    if (s & 4) v = make_uint4(v.z, v.w, 0u, 0u);
+    return s & 8 ? make_uint4(0u, 0u, 0u, 0u) : v;
+}
 
 // ---- rows that start anywhere
 
@@ -569,7 +577,8 @@ __device__ __forceinline__ void shift_run(const T *row, uint4 (&v)[U], unsigned 
 
 // 16 MB rows by 16 NB columns of y a workgroup, its wavefronts each with a range of the depth and operands straight from
 // memory into the matrix instructions; their sums meet in LDS.  Rows may start at any element.  A wavefront has U steps of 32
-// of the depth in flight: what bounds the form is how long memory takes to answer, so everything is asked for at once.
+// of the depth in flight: what bounds the form is how long memory takes to answer, so everything is asked for at once.  K is
+// 8 or more.
 template <typename T, typename TO, ActCode A, int MB, int NB, int WAVES, bool ODD>
 __global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
     constexpr int U = 4, ITEMS = MB * NB * 64;
@@ -628,21 +637,46 @@ __global__ __launch_bounds__(64 * WAVES) void direct_kernel(Params p) {
 #pragma unroll
                 for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[j][u], b[i][u], acc[i][j], T());
     }
-    if (k - 8 * (lane >> 4) < k1) {   // the rest, its last chunk perhaps short
+    // The rest.  Of a chunk that the row's end cuts the row's last eight elements are loaded instead and moved down; chunks
+    // behind the range load whatever is there for nothing.
+    const int kb = k - 8 * (lane >> 4);
+    if (kb < k1) {
         uint4 a[U][NB], b[U][MB];
+        unsigned at[U][NB], bt[U][MB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (kb + 32 * u >= k1) continue;
+            const int from = min(k + 32 * u, p.K - 8);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) a[u][j] = load_cut(wr[j], k + 32 * u, k1);
+            for (int j = 0; j < NB; ++j) {
+                if constexpr (ODD) a[u][j] = load_floor(wr[j] + from), at[u][j] = load_tail(wr[j] + from);
+                else __builtin_memcpy(&a[u][j], wr[j] + from, 16);
+            }
 #pragma unroll
-            for (int i = 0; i < MB; ++i) b[u][i] = load_cut(xr[i], k + 32 * u, k1);
+            for (int i = 0; i < MB; ++i) {
+                if constexpr (ODD) b[u][i] = load_floor(xr[i] + from), bt[u][i] = load_tail(xr[i] + from);
+                else __builtin_memcpy(&b[u][i], xr[i] + from, 16);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (kb + 32 * u >= k1) continue;
+            const int from = min(k + 32 * u, p.K - 8), less = min(max(k + 32 * u + 8 - k1, 0), 8);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                if constexpr (ODD) a[u][j] = shift_in(a[u][j], at[u][j], wr[j] + from);
+                a[u][j] = drop(a[u][j], less);
+            }
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                if constexpr (ODD) b[u][i] = shift_in(b[u][i], bt[u][i], xr[i] + from);
+                b[u][i] = drop(b[u][i], less);
+            }
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
                 for (int j = 0; j < NB; ++j) acc[i][j] = mma(a[u][j], b[u][i], acc[i][j], T());
+        }
     }
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -1035,8 +1069,8 @@ MatmulChoice choose_matmul(const MatmulArgs &a, int n_cu) {
             best = c;
         }
     };
-    consider({MatmulForm::DIRECT, 1, false}, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
-    consider({MatmulForm::DIRECT22, 1, false}, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
+    if (a.K >= 8) consider({MatmulForm::DIRECT, 1, false}, ring_cost(kDirect, a, n_cu, odd ? 1.25 : 1.0));
+    if (a.K >= 8) consider({MatmulForm::DIRECT22, 1, false}, ring_cost(kDirect22, a, n_cu, odd ? 1.25 : 1.0));
     const size_t room = pack_bytes(a);
     if (t > kPack && room <= ws_bytes && room < (1ull << 34)) {   // chunks are counted below 2^30
         MatmulArgs b = a;
