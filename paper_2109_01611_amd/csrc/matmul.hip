@@ -10,13 +10,13 @@
 //   tile     64x64, 128x64 and 128x128 tiles that a workgroup goes through slice by slice.  Bound by the rate at which a CU
 //            takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128 56 us, 933 TFLOP/s.
 //            The 64x64 one also with a depth that up to eight workgroups share, whose sums meet in the workspace: tall y with
-//            few tiles and a long depth (1742 x 216 x 3816 16.3 us, in rings 20.4).
+//            few tiles and a long depth (1742 x 216 x 3816 15.7 us, in rings 20.3).
 //   big      256x256 tiles, 160 KB of LDS: as many matrix instructions as transfers can feed.  8192 x 4096 x 4096 216 us,
 //            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 1.33.
 //   direct,  rows that do not start at multiples of 16 bytes or a depth that is not a multiple of 8: operands go from memory
 //   staged   into the matrix instructions (few rows, few tiles), or through registers into LDS (64x64 tiles).
 //            200 x 300 x 4001 9.6 us.  Larger products of such operands lay them out anew in the workspace first and
-//            take the forms above: 2048 x 1024 x 1001 18.5 us (staged 23.2), 4096 x 4096 x 1022 50.5 (88.1).
+//            take the forms above: 2048 x 1024 x 1001 16.3 us (staged 22.5), 4096 x 4096 x 1022 46 (84).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -60,7 +60,7 @@ struct Params {
 
 // What the epilogue adds to NC consecutive columns of row m, asked for before it is needed: a workgroup with a short depth
 // lives about as long as these loads take.  Rows of y and the residual may start anywhere: 16 bytes at a time they cost less
-// than element by element at any alignment (12965 x 3053 x 280 fp16 153 us element by element, 62 so).
+// than element by element at any alignment (12965 x 3053 x 280 bf16 153 us element by element, 65 so).
 template <int NC>
 __device__ __forceinline__ void load_bias(const Params &p, int n, float (&b)[NC]) {
 #pragma unroll
@@ -800,13 +800,13 @@ __global__ __launch_bounds__(64 * WAVES) void ring_kernel(Params p) {
 
 // ---- rows laid out anew
 
-// Rows of K elements that start anywhere -> rows of Kp, a multiple of 8, that start at multiples of 16 bytes, with zeros behind
-// the last element; up to two operands.
+// Rows of K elements that start anywhere -> rows of Kp, a multiple of 8, with zeros behind the last element; up to two
+// operands.
 struct Pack {
     const void *src[2];
     void *dst[2];
     int ld[2];
-    int K, Kp;
+    int K, Kp, pitch;      // pitch: from row to row of what is written
     int first, items;      // chunks of 8 elements of the first operand and of both
     FastDiv d_chunks;      // by Kp / 8
 };
@@ -828,7 +828,7 @@ __global__ __launch_bounds__(256) void pack_kernel(Pack p) {
     if (last) behind = tail;
     if (whole) v = shift_in(v, behind, r + k);
     else if (in) v = load_cut(r, k, p.K);
-    if (in) *reinterpret_cast<uint4 *>(static_cast<T *>(p.dst[which]) + static_cast<long long>(row) * p.Kp + k) = v;
+    if (in) *reinterpret_cast<uint4 *>(static_cast<T *>(p.dst[which]) + static_cast<long long>(row) * p.pitch + k) = v;
 }
 
 // ---- a depth that several workgroups share
@@ -917,12 +917,15 @@ double ring_cost(const RingCost &c, const MatmulArgs &a, int n_cu, double slower
 }
 
 int padded(int K) { return (K + 7) / 8 * 8; }
+// Rows laid out anew start at multiples of 128 bytes, so that a transfer of 128 takes one line: in rows of 4784 elements
+// 8042 x 2992 x 4778 took 339 us, in rows of 4800 288.
+int pitch(int K) { return (K + 63) / 64 * 64; }
 // The transfers to LDS bring aligned 16 bytes.
 bool x_aligned(const MatmulArgs &a) { return reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx % 8 == 0 && a.K % 8 == 0; }
 bool w_aligned(const MatmulArgs &a) { return reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && a.ldw % 8 == 0 && a.K % 8 == 0; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-size_t pack_x_bytes(const MatmulArgs &a) { return x_aligned(a) ? 0 : round256(2ull * a.M * padded(a.K)); }
-size_t pack_w_bytes(const MatmulArgs &a) { return w_aligned(a) ? 0 : round256(2ull * a.N * padded(a.K)); }
+size_t pack_x_bytes(const MatmulArgs &a) { return x_aligned(a) ? 0 : round256(2ull * a.M * pitch(a.K)); }
+size_t pack_w_bytes(const MatmulArgs &a) { return w_aligned(a) ? 0 : round256(2ull * a.N * pitch(a.K)); }
 size_t pack_bytes(const MatmulArgs &a) { return pack_x_bytes(a) + pack_w_bytes(a); }
 // Some row of x or w may not start at a multiple of 4 bytes.
 bool rows_odd(const MatmulArgs &a) {
@@ -1092,6 +1095,7 @@ hipError_t launch_matmul(const MatmulArgs &args, const LaunchCtx &ctx, hipStream
         Pack k{};
         k.K = a.K;
         k.Kp = padded(a.K);
+        k.pitch = pitch(a.K);
         const int chunks = k.Kp / 8;
         k.d_chunks = make_fastdiv(chunks);
         auto add = [&](const void *src, int ld, int rows, size_t bytes) -> const void * {
@@ -1106,8 +1110,8 @@ hipError_t launch_matmul(const MatmulArgs &args, const LaunchCtx &ctx, hipStream
         const size_t xb = pack_x_bytes(a), wb = pack_w_bytes(a);
         a.x = add(a.x, a.ldx, a.M, xb);
         a.w = add(a.w, a.ldw, a.N, wb);
-        if (xb) a.ldx = k.Kp;
-        if (wb) a.ldw = k.Kp;
+        if (xb) a.ldx = k.pitch;
+        if (wb) a.ldw = k.pitch;
         a.K = k.Kp;
         const dim3 grid((static_cast<unsigned>(k.items) + 255) / 256);
         if (a.dtype == GPULET_BF16) pack_kernel<__bf16><<<grid, 256, 0, stream>>>(k);
