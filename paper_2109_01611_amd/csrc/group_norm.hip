@@ -292,6 +292,8 @@ __device__ __forceinline__ Stat join_lanes(Stat s, int lanes) {
 constexpr int batch_of(int unit_bytes) { return unit_bytes >= 8 ? 4 : 8; }
 
 // A thread's walk over the pixels of a chunk, batch_of(UB) units at a time: `full` batches without a test, then one with.
+// Steps to pixels behind the chunk may be longer than the image, so nothing is added to the offset of a unit that is left
+// out: OOB and such a step in one sum may come out inside the image, and a scalar offset has to stay below the buffer's size.
 template <typename T, int V>
 struct Walk {
     static constexpr int UB = V * static_cast<int>(sizeof(T)), B = batch_of(UB);
@@ -313,8 +315,12 @@ struct Walk {
             for (int i = 0; i < B; ++i) v[i] = load_unit<UB>(rs, o, i * d);
         } else {
 #pragma unroll
-            for (int i = 0; i < B; ++i) v[i] = load_unit<UB>(rs, valid(i) ? o : OOB, i * d);
+            for (int i = 0; i < B; ++i) v[i] = load_unit<UB>(rs, valid(i) ? o : OOB, i * p.R < left ? i * d : 0u);
         }
+    }
+    // Vector offset of unit i for a store, `whole` where its batch is full and the thread has a unit.
+    __device__ __forceinline__ unsigned store_at(int i, bool whole, unsigned o, unsigned d) const {
+        return whole || valid(i) ? o + i * d : OOB;
     }
     __device__ __forceinline__ void next() {
         q += B * p.R;
@@ -434,7 +440,7 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
 #pragma unroll
         for (int i = 0; i < W::B; ++i) {
             const typename W::Raw y = finish_unit<T, V, A>(xv[i], p.r ? rv[i] : xv[i], p.r != nullptr, mean, a, b, p.act);
-            store_unit<W::UB, NT>(ys, whole || w.valid(i) ? o : OOB, i * d, y);
+            store_unit<W::UB, NT>(ys, w.store_at(i, whole, o, d), 0u, y);
         }
         w.next();
         if (w.left <= 0) break;

@@ -1,0 +1,45 @@
+"""Group norm where its arithmetic comes to an end: steps longer than an image, and maps of one pixel."""
+
+import pytest
+import torch
+
+from paper_2109_01611_amd import gpulet
+
+from test_gpu_group_norm import GUARD, Case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("which", ["x", "residual", "y"])
+@pytest.mark.parametrize("pixels", [1, 2])
+def test_pixels_further_apart_than_memory_is_long(which, pixels):
+    # One pixel, or two, and a distance between pixels of up to 2^31 bytes: the other pixels of a batch of loads and stores
+    # do not exist, and nothing may come of their offsets, which pass 32 bits.
+    C, far = 8208, 1 << (29 if pixels == 1 else 15)
+    c = Case(21, 1, 1, pixels, C, 1, act="relu", res=True, pad=(0, 0, 0))
+    ld = dict(x=C, residual=C, y=C)
+    ld[which] = far
+    room = torch.full(((pixels - 1) * far + C + 4096,), GUARD, dtype=torch.bfloat16, device=DEV)
+    src = dict(x=c.x, residual=c.r, y=c.y)
+    for p in range(pixels):
+        room[p * far:p * far + C].copy_(src[which][0, 0, p])
+    at = {k: v.data_ptr() for k, v in src.items()}
+    at[which] = room.data_ptr()
+    d = gpulet.group_norm_desc(at["x"], c.gamma, c.beta, at["y"], 1, C, 1, pixels, 1, eps=c.eps, act=gpulet.ACT_RELU,
+                               residual=at["residual"], x_ch_stride=ld["x"], r_ch_stride=ld["residual"], y_ch_stride=ld["y"])
+    size = gpulet.group_norm_workspace_bytes(d)
+    assert size > 0                       # the form of two launches
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    gpulet.group_norm(d, ws, size)
+    torch.cuda.synchronize()
+    if which == "y":
+        for p in range(pixels):
+            c.y[0, 0, p].copy_(room[p * far:p * far + C])
+            room[p * far:p * far + C] = GUARD
+    else:
+        for p in range(pixels):
+            room[p * far:p * far + C] = GUARD
+    assert bool((room == GUARD).all())
+    c.check(which)
