@@ -269,7 +269,8 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
     });
 }
 
-// Joins the statistics (count, mean, sum of squared differences) of two disjoint sets; an empty one counts for nothing.
+// Joins the statistics (count, mean, sum of squared differences) of two disjoint sets; an empty one, whose mean is zero,
+// counts for nothing.  d * d alone may be more than fp32 holds where one set is empty and the other's mean is large.
 struct Stat {
     float n, mean, m2;
 };
@@ -277,7 +278,7 @@ __device__ __forceinline__ Stat join(const Stat a, const Stat b) {
     const float n = a.n + b.n;
     const float f = a.n > 0.f ? b.n * __builtin_amdgcn_rcpf(n) : 1.f;   // equal means stay what they are, to the bit
     const float d = b.mean - a.mean;
-    return Stat{n, a.mean + d * f, a.m2 + b.m2 + d * d * a.n * f};
+    return Stat{n, a.mean + d * f, a.m2 + b.m2 + d * (a.n * f) * d};
 }
 template <int STEP = 0>
 __device__ __forceinline__ Stat join_lanes(Stat s, int lanes) {

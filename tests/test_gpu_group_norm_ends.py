@@ -43,3 +43,16 @@ def test_pixels_further_apart_than_memory_is_long(which, pixels):
             room[p * far:p * far + C] = GUARD
     assert bool((room == GUARD).all())
     c.check(which)
+
+# ---- everything below: N, H, W, C, groups; the first of each list is held in registers, the others take two launches
+FORMS = [(2, 9, 9, 64, 8), (1, 64, 64, 320, 32), (1, 150, 150, 64, 1), (1, 1, 3, 8200, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", FORMS, ids=str)
+def test_constant_groups_of_any_size(size, dtype):
+    for value in (2e19, -3e30, 1e38, 1e-30):
+        c = Case(6, *size, dtype=dtype, act="relu", res=True)
+        c.x.fill_(value)
+        want = torch.relu(c.beta + c.r.float()).to(c.dt)
+        assert torch.equal(c.run(), want), value
