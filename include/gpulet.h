@@ -537,6 +537,10 @@ gpulet_status gpulet_matmul(const gpulet_matmul_desc *d, void *workspace, size_t
  * it is part of or on the gpu-let.  An infinity or NaN makes its group's
  * outputs in its image NaN and reaches no other group or image.  A group whose
  * values are all equal gives act(beta + residual); with eps = 0 its outputs are NaN.
+ * Where a group's squared differences add up to more than fp32 holds (never
+ * while |x| stays below 2^47) its variance counts as infinite: its outputs are
+ * act(beta + residual), or NaN if the sum of the differences overflows as well
+ * (never while |x| stays below 2^96).
  * y may be x itself or the residual itself (same address, ch_stride); otherwise y
  * may share no element with x, residual, gamma or beta.
  * Errors: GPULET_EINVAL for a NULL descriptor, x or y; non-positive sizes; groups

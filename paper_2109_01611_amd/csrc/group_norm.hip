@@ -380,7 +380,8 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     const float shift = cnt > 0.f ? sum / cnt : 0.f;
     part[0][threadIdx.x] = cnt;
     part[1][threadIdx.x] = k0 + shift;
-    part[2][threadIdx.x] = fmaxf(sq - sum * shift, sq * 0.f);   // not below zero, and NaN where sq is not finite
+    // not below zero; where the squares overflow, infinite, as their sum is in the other form (not infinity less infinity)
+    part[2][threadIdx.x] = sq < __builtin_inff() ? fmaxf(sq - sum * shift, 0.f) : sq;
     __syncthreads();
     const int sub = threadIdx.x & (p.lanes - 1);
     for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {

@@ -44,6 +44,7 @@ def test_pixels_further_apart_than_memory_is_long(which, pixels):
     assert bool((room == GUARD).all())
     c.check(which)
 
+
 # ---- everything below: N, H, W, C, groups; the first of each list is held in registers, the others take two launches
 FORMS = [(2, 9, 9, 64, 8), (1, 64, 64, 320, 32), (1, 150, 150, 64, 1), (1, 1, 3, 8200, 1)]
 
@@ -56,3 +57,13 @@ def test_constant_groups_of_any_size(size, dtype):
         c.x.fill_(value)
         want = torch.relu(c.beta + c.r.float()).to(c.dt)
         assert torch.equal(c.run(), want), value
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", FORMS, ids=str)
+def test_squared_differences_past_fp32(size, dtype):
+    # the variance counts as infinite, whichever form runs
+    for scale in (1e20, 1e25):
+        c = Case(7, *size, dtype=dtype, act="relu", res=True, scale=scale)
+        want = torch.relu(c.beta + c.r.float()).to(c.dt)
+        assert torch.equal(c.run(), want), scale
