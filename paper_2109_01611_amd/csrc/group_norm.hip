@@ -274,12 +274,13 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
 struct Stat {
     float n, mean, m2;
 };
-__device__ __forceinline__ Stat join(const Stat a, const Stat b) {
+// `d`: how far b's mean is from a's.
+__device__ __forceinline__ Stat join(const Stat a, const Stat b, float d) {
     const float n = a.n + b.n;
     const float f = a.n > 0.f ? b.n * __builtin_amdgcn_rcpf(n) : 1.f;   // equal means stay what they are, to the bit
-    const float d = b.mean - a.mean;
     return Stat{n, a.mean + d * f, a.m2 + b.m2 + d * (a.n * f) * d};
 }
+__device__ __forceinline__ Stat join(const Stat a, const Stat b) { return join(a, b, b.mean - a.mean); }
 template <int STEP = 0>
 __device__ __forceinline__ Stat join_lanes(Stat s, int lanes) {
     if ((1 << STEP) >= lanes) return s;
@@ -329,9 +330,12 @@ struct Walk {
     }
 };
 
-// Statistics of one chunk of an image for the groups of a workgroup.  A thread sums differences from its first value and
-// their squares.  That value need not be near the mean: where it is D away, a fraction 1 / n of the thread's n values is,
-// the squared differences' sum is at least about D^2 and the roundings of n D^2 are n 2^-24 of it.
+// Statistics of one chunk of an image for the groups of a workgroup.  A thread sums the differences of a batch from the mean
+// of what it summed before, and their squares, and joins the batch's statistics to those before; the first batch's are
+// from its own mean.  The roundings of the squares' sum are at most B V 2^-24 of it, and of the n0 + nb differences
+// joined so far, the nb new ones, whose mean is D away, add n0 nb / (n0 + nb) D^2, at least half of what their
+// squares' sum has from D: the roundings are no more than 2 B V 2^-24 (4e-6) of the result, wherever the values lie.
+// (One sum of differences from the thread's first value: up to 1e-2 of it where that value is the only one that lies far off.)
 template <typename T, int V>
 __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     typedef Walk<T, V> W;
@@ -347,41 +351,52 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     W w(p, at, q0, q1);
     typename W::Raw xv[W::B];
     w.load(xs, p.ldx, xv);
-    const float cnt = at.in && q0 + at.row < q1 ? static_cast<float>((q1 - q0 - at.row + p.R - 1) / p.R * V) : 0.f;
+    // Calls f with every value of a batch, or with `none` for one that is not there.  -> how many are there
+    auto each = [&](const typename W::Raw (&raw)[W::B], bool whole, float none, auto &&f) {
+        int units = whole && at.in ? W::B : 0;
+#pragma unroll
+        for (int i = 0; i < W::B; ++i) {
+            const bool ok = whole || w.valid(i);
+            if (!whole) units += ok;
+            float v[V];
+            unpack<T, V>(raw[i], v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f(ok ? v[j] : none);
+        }
+        return static_cast<float>(units * V);
+    };
     float first[V];
     unpack<T, V>(xv[0], first);
-    const float k0 = first[0];
-    float sum = 0.f, sq = 0.f;
+    float sum = 0.f;
+    float nb = each(xv, w.full(), first[0], [&](float v) { sum += v - first[0]; });
+    // of equal values the mean is that value, to the bit; of none it is zero
+    Stat all{0.f, first[0] + sum * __builtin_amdgcn_rcpf(fmaxf(nb, 1.f)), 0.f};
     while (true) {
         typename W::Raw cur[W::B];
-        const bool whole = w.full();
-        bool ok[W::B];
 #pragma unroll
-        for (int i = 0; i < W::B; ++i) {
-            cur[i] = xv[i];
-            ok[i] = whole || w.valid(i);
-        }
-        w.next();
-        const bool more = w.left > 0;
-        if (more) w.load(xs, p.ldx, xv);   // on its way while the batch before is summed
-#pragma unroll
-        for (int i = 0; i < W::B; ++i) {
-            float f[V];
-            unpack<T, V>(cur[i], f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = ok[i] ? f[j] - k0 : 0.f;
-                sum += d;
-                sq += d * d;
-            }
-        }
+        for (int i = 0; i < W::B; ++i) cur[i] = xv[i];
+        W next = w;
+        next.next();
+        const bool more = next.left > 0;
+        if (more) next.load(xs, p.ldx, xv);   // on its way while the batch before is summed
+        float sq = 0.f;
+        sum = 0.f;
+        nb = each(cur, w.full(), all.mean, [&](float v) {
+            const float d = v - all.mean;
+            sum += d;
+            sq += d * d;
+        });
+        const float d = sum * __builtin_amdgcn_rcpf(fmaxf(nb, 1.f));
+        // not below zero; where the squares overflow, infinite, as their sum is in the other form (not infinity less infinity)
+        const float m2 = sq < __builtin_inff() ? fmaxf(sq - sum * d, 0.f) : sq;
+        all = join(all, Stat{nb, all.mean + d, m2}, d);
+        w.q = next.q;
+        w.left = next.left;
         if (!more) break;
     }
-    const float shift = cnt > 0.f ? sum / cnt : 0.f;
-    part[0][threadIdx.x] = cnt;
-    part[1][threadIdx.x] = k0 + shift;
-    // not below zero; where the squares overflow, infinite, as their sum is in the other form (not infinity less infinity)
-    part[2][threadIdx.x] = sq < __builtin_inff() ? fmaxf(sq - sum * shift, 0.f) : sq;
+    part[0][threadIdx.x] = all.n;
+    part[1][threadIdx.x] = all.mean;
+    part[2][threadIdx.x] = all.m2;
     __syncthreads();
     const int sub = threadIdx.x & (p.lanes - 1);
     for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {

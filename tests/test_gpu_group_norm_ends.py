@@ -3,9 +3,11 @@
 import pytest
 import torch
 
+import block_reference as ref
+import norm_bounds
 from paper_2109_01611_amd import gpulet
 
-from test_gpu_group_norm import GUARD, Case
+from test_gpu_group_norm import GUARD, Case, _np
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -49,6 +51,13 @@ def test_pixels_further_apart_than_memory_is_long(which, pixels):
 FORMS = [(2, 9, 9, 64, 8), (1, 64, 64, 320, 32), (1, 150, 150, 64, 1), (1, 1, 3, 8200, 1)]
 
 
+def _close(c, what):
+    y, err = norm_bounds.group_norm(_np(c.x), None if c.gamma is None else _np(c.gamma), None if c.beta is None else _np(c.beta),
+                                    c.G, c.eps, None if c.r is None else _np(c.r), c.act)
+    ref.assert_within(_np(c.y), y, ref.rounded_bound(y, err, c.dt, c.act), what)
+    c.check_guards()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("size", FORMS, ids=str)
 def test_constant_groups_of_any_size(size, dtype):
@@ -67,3 +76,23 @@ def test_squared_differences_past_fp32(size, dtype):
         c = Case(7, *size, dtype=dtype, act="relu", res=True, scale=scale)
         want = torch.relu(c.beta + c.r.float()).to(c.dt)
         assert torch.equal(c.run(), want), scale
+
+
+OUTLIERS = FORMS[1:] + [(1, 256, 256, 64, 1), (2, 200, 200, 40, 2), (1, 300, 300, 24, 1)]
+
+
+@pytest.mark.parametrize("size", OUTLIERS, ids=str)
+def test_first_values_far_from_the_others(size):
+    # Sums of differences from a first value that lies far off: their roundings may not be those of the far value's size
+    # times their number.  A 256 x 256 x 64 map in fp32 is summed in pieces of 1024 pixels, whose first 32 have the first values.
+    N, H, W, C, G = size
+    for every, first in ((H * W, 1), (H * W, 32), (1024, 32), (768, 32), (64, 1)):
+        for step in (4, C // G):
+            c = Case(8, *size, dtype="f32", scale=0.01)
+            px = c.x.reshape(N, H * W, C).clone()
+            at = torch.arange(H * W, device=DEV) % every < first
+            ch = torch.arange(C, device=DEV) % step == 0
+            px[:, at[:, None] & ch[None, :]] = 1234.5678
+            c.x.copy_(px.view(N, H, W, C))
+            c.run()
+            _close(c, (every, first, step))
