@@ -114,41 +114,50 @@ __device__ __forceinline__ float other_half(float f) {
     }
 }
 
-// Sum over the first `lanes` (a power of two), the second, ... lanes of a wavefront.
-template <int STEP = 0>
-__device__ __forceinline__ float lane_sum(float v, int lanes) {
-    if ((1 << STEP) >= lanes) return v;
-    v += other_half<STEP>(v);
-    if constexpr (STEP < 5) return lane_sum<STEP + 1>(v, lanes);
-    return v;
+// Sums over the first `lanes` (a power of two), the second, ... lanes of a wavefront.
+template <int K, int STEP = 0>
+__device__ __forceinline__ void lane_sums(float (&v)[K], int lanes) {
+    if ((1 << STEP) >= lanes) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += other_half<STEP>(v[k]);
+    if constexpr (STEP < 5) lane_sums<K, STEP + 1>(v, lanes);
 }
 
-// Sum of `v` over the threads of the calling thread's group; threads of no unit pass zero.  `part`: one float per thread
-// of LDS, `res`: kMaxGb floats, neither in use by anybody else.  The order of the sum depends on nothing but the geometry.
-__device__ __forceinline__ float group_sum(float v, const Params &p, int my_group, float *part, float *res) {
+// Replaces each of the K values by its sum over the threads of the calling thread's group; threads of no unit pass zero.
+// `part`: K floats per thread of LDS, `res`: K per group or wavefront, neither in use by anybody else; `part` is free again on
+// return.  The order of the sum depends on nothing but the geometry.
+template <int K>
+__device__ __forceinline__ void group_sums(float (&v)[K], const Params &p, int my_group, float (*part)[K], float (*res)[K]) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     if (p.gb == 1) {
-        v = lane_sum(v, 64);
-        if (lane == 0) res[wave] = v;
+        lane_sums(v, 16);   // within rows; the rows' sums go through scalar registers, which takes no trip to LDS
+        auto row = [](float f, int r) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), 16 * r)); };
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = (row(v[k], 0) + row(v[k], 1)) + (row(v[k], 2) + row(v[k], 3));
+        if (lane == 0) __builtin_memcpy(res[wave], v, sizeof(v));
         __syncthreads();
-        float s = 0.f;
-        for (int i = 0; i < waves; ++i) s += res[i];
-        return s;
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = 0.f;
+        for (int i = 0; i < waves; ++i)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += res[i][k];
+        return;
     }
-    part[threadIdx.x] = v;
+    __builtin_memcpy(part[threadIdx.x], v, sizeof(v));
     __syncthreads();
     const int sub = threadIdx.x & (p.lanes - 1);
     for (int g = threadIdx.x / p.lanes; g < p.gb; g += blockDim.x / p.lanes) {
-        float s = 0.f;
+        float s[K] = {};
         for (int i = sub; i < p.R * p.ug; i += p.lanes) {
             const int row = fdiv(i, p.d_ug);
-            s += part[row * p.upx + g * p.ug + (i - row * p.ug)];
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[k] += part[row * p.upx + g * p.ug + (i - row * p.ug)][k];
         }
-        s = lane_sum(s, p.lanes);
-        if (sub == 0) res[g] = s;
+        lane_sums(s, p.lanes);
+        if (sub == 0) __builtin_memcpy(res[g], s, sizeof(s));
     }
     __syncthreads();
-    return res[my_group];
+    __builtin_memcpy(v, res[my_group], sizeof(v));
 }
 
 // The unit of a thread: its row among the R pixels covered at once (or none), its channels and their scale and shift.
@@ -200,7 +209,9 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
     constexpr int UB = V * static_cast<int>(sizeof(T));
     typedef typename RawUnit<UB>::Type Raw;
     constexpr bool EARLY_RES = NR * UB <= 64;   // the residual, too, is requested before the statistics
-    __shared__ float part[kMaxThreads], res1[kMaxGb], res2[kMaxGb];
+    extern __shared__ float2 part[];   // one per thread where the workgroup has several groups (held_lds), for both sums
+    __shared__ float res1[kMaxGb][1];
+    __shared__ __attribute__((aligned(8))) float res2[kMaxGb][2];
     const int id = die_block(p.per_die, blockIdx.x);
     if (id >= p.total) return;
     const int n = fdiv(id, p.d_ncb), c0 = (id - n * p.n_cb) * p.cb;
@@ -233,32 +244,45 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
     if constexpr (EARLY_RES) {
         if (p.r) units([&](int i) { rv[i] = load_unit<UB>(rs, valid(i) ? ro : OOB, step(i, p.ldr)); });
     }
-    // Sums are of differences from the group's first value: of a group of equal values the mean is that value, to the bit.
+    // Of a group of equal values the mean is that value, to the bit: sums are of differences from its first value.  That one
+    // may lie so far off that the roundings of such a sum count (16x16x32 fp32, one value far off: 4.5e-6 of a standard
+    // deviation).  So it only gives `near`, the mean of some of the group's values, and the differences from that give what
+    // is missing to the mean.  One value in twelve, at least, is enough: their mean is at most sqrt(11) standard deviations
+    // away from that of all, where the squares' sum, with its 30 roundings, is twelve times the variance's.
     float first[1];
     unpack<T, 1>(load_unit<sizeof(T)>(xs, static_cast<unsigned>(at.group * p.cg) * static_cast<unsigned>(sizeof(T))), first);
     float a[V], b[V];
     load_affine<V>(p, c0 + (at.in ? at.c : 0), a, b);
-    const float inv = 1.f / (static_cast<float>(p.HW) * static_cast<float>(p.cg));
-    float s = 0.f;
-    units([&](int i) {
+    constexpr int SUB = (NR + 3) / 4, SV = V < 2 ? V : 2;   // units and values of each
+    float s[1] = {};
+#pragma unroll
+    for (int i = 0; i < SUB; ++i) {
         float f[V];
         unpack<T, V>(xv[i], f);
         float t = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) t += f[j] - first[0];
-        s += valid(i) ? t : 0.f;
-    });
-    const float mean = first[0] + group_sum(s, p, at.group, part, res1) * inv;
-    s = 0.f;
+        for (int j = 0; j < SV; ++j) t += f[j] - first[0];
+        s[0] += valid(i) ? t : 0.f;
+    }
+    group_sums(s, p, at.group, reinterpret_cast<float(*)[1]>(part), res1);
+    const float near = first[0] + s[0] * __builtin_amdgcn_rcpf(static_cast<float>(min(p.HW, SUB * p.R)) * static_cast<float>(p.gu * SV));
+    const float inv = __builtin_amdgcn_rcpf(static_cast<float>(p.HW) * static_cast<float>(p.cg));
+    float d[2] = {};
     units([&](int i) {
         float f[V];
         unpack<T, V>(xv[i], f);
-        float t = 0.f;
+        float t = 0.f, q = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) t += (f[j] - mean) * (f[j] - mean);
-        s += valid(i) ? t : 0.f;
+        for (int j = 0; j < V; ++j) {
+            t += f[j] - near;
+            q += (f[j] - near) * (f[j] - near);
+        }
+        d[0] += valid(i) ? t : 0.f;
+        d[1] += valid(i) ? q : 0.f;
     });
-    const float var = group_sum(s, p, at.group, part, res2) * inv;
+    group_sums(d, p, at.group, reinterpret_cast<float(*)[2]>(part), res2);
+    const float more = d[0] * inv, mean = near + more;
+    const float var = d[1] < __builtin_inff() ? fmaxf(d[1] * inv - more * more, 0.f) : d[1];
     const float rstd = 1.f / __builtin_sqrtf(var + p.eps);
 #pragma unroll
     for (int j = 0; j < V; ++j) a[j] *= rstd;
@@ -588,13 +612,17 @@ Plan make_plan(const GroupNormArgs &a) {
     return pl;
 }
 
+// LDS of a held kernel's sums per thread: as many workgroups of 64 threads as a CU takes have room.
+size_t held_lds(const Params &p) { return p.gb > 1 ? p.threads * sizeof(float2) : 0; }
+
 template <typename T, int V, ActCode A>
 hipError_t launch_units(const Plan &pl, hipStream_t stream) {
     const dim3 grid(8 * pl.p.per_die), block(pl.p.threads);
     constexpr int UD = V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1;   // dwords of a unit
     if (pl.form == Plan::HELD) {
-        if (pl.iters * UD <= 8) held_kernel<T, V, 8 / UD, A><<<grid, block, 0, stream>>>(pl.p);
-        else held_kernel<T, V, kHeldDwords / UD, A><<<grid, block, 0, stream>>>(pl.p);
+        const size_t lds = held_lds(pl.p);
+        if (pl.iters * UD <= 8) held_kernel<T, V, 8 / UD, A><<<grid, block, lds, stream>>>(pl.p);
+        else held_kernel<T, V, kHeldDwords / UD, A><<<grid, block, lds, stream>>>(pl.p);
         return hipGetLastError();
     }
     stats_kernel<T, V><<<grid, block, 0, stream>>>(pl.p);

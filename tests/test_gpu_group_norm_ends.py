@@ -78,7 +78,7 @@ def test_squared_differences_past_fp32(size, dtype):
         assert torch.equal(c.run(), want), scale
 
 
-OUTLIERS = FORMS[1:] + [(1, 256, 256, 64, 1), (2, 200, 200, 40, 2), (1, 300, 300, 24, 1)]
+OUTLIERS = FORMS + [(1, 16, 16, 32, 1), (1, 7, 7, 160, 1), (3, 5, 13, 48, 4), (1, 256, 256, 64, 1), (2, 200, 200, 40, 2), (1, 300, 300, 24, 1)]
 
 
 @pytest.mark.parametrize("size", OUTLIERS, ids=str)
