@@ -39,6 +39,7 @@ struct Step {
     const float *b;
     gpulet_group_norm_desc norm;                     // GROUP_NORM, tensors filled in at run time
     gpulet_matmul_desc mm;                           // MATMUL, likewise
+    bool scratch;           // GROUP_NORM, MATMUL: may use the scratch behind the buffers
     bool slice;             // CONV writing a channel slice of a wider (concatenated) tensor
     bool slice2;            // the same for the second buffer
     int group_len;          // CONV: layers launched together starting here (1: alone; 0: inside a group)
@@ -74,7 +75,8 @@ std::atomic<int> g_model_lanes{1};
 // Buffers are reused, so besides "reads what an earlier layer wrote" a layer must also wait
 // for every earlier reader and writer of the buffer it overwrites.  Layers that write
 // disjoint channel slices of one concatenated tensor do not depend on one another, but each
-// of them depends on whatever the first of them had to wait for (`guard`).
+// of them depends on whatever the first of them had to wait for (`guard`).  The scratch behind the
+// buffers counts as a buffer that every layer which may use it overwrites.
 //
 // A layer stays on the lane of its most recent dependency when it is the first to continue
 // that lane; otherwise it moves to the lane that has been idle longest.  Dependencies on the
@@ -84,7 +86,7 @@ void assign_lanes(Plan &plan, int n_bufs, int n_lanes) {
         std::vector<int> writers, readers, guard;
         bool sliced = false;
     };
-    std::vector<Hazard> hz(static_cast<size_t>(n_bufs));
+    std::vector<Hazard> hz(static_cast<size_t>(n_bufs) + 1);   // the last: the scratch
     std::vector<int> tail(static_cast<size_t>(n_lanes), -1);  // last layer placed on each lane
     const int n = static_cast<int>(plan.steps.size());
     for (int i = 0; i < n; ++i) {
@@ -113,6 +115,7 @@ void assign_lanes(Plan &plan, int n_bufs, int n_lanes) {
         writes(s.out_buf, s.slice);
         if (s.out2_buf >= 0) writes(s.out2_buf, s.slice2);
         if (s.pool_buf >= 0) writes(s.pool_buf, false);
+        if (s.scratch) writes(n_bufs, false);
         std::sort(deps.begin(), deps.end());
         deps.erase(std::unique(deps.begin(), deps.end()), deps.end());
 
@@ -149,6 +152,7 @@ void assign_lanes(Plan &plan, int n_bufs, int n_lanes) {
         hz[static_cast<size_t>(s.out_buf)].writers.push_back(i);
         if (s.out2_buf >= 0) hz[static_cast<size_t>(s.out2_buf)].writers.push_back(i);
         if (s.pool_buf >= 0) hz[static_cast<size_t>(s.pool_buf)].writers.push_back(i);
+        if (s.scratch) hz[static_cast<size_t>(n_bufs)].writers.push_back(i);
     }
 }
 
@@ -342,7 +346,9 @@ gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
                     const gpulet_status st = check_group_norm(&s.norm, a);
                     if (st != GPULET_OK) return st;
                     if (align != 256) a.x = stand_in(1, align);
-                    plan.op_bytes = std::max(plan.op_bytes, group_norm_workspace(a));
+                    const size_t need = group_norm_workspace(a);
+                    s.scratch = s.scratch || need > 0;
+                    plan.op_bytes = std::max(plan.op_bytes, need);
                 }
             } else {
                 if (1LL * batch * src.H * src.W > INT_MAX) return GPULET_EINVAL;
@@ -352,6 +358,7 @@ gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
                 const gpulet_status st = check_matmul(&s.mm, a);
                 if (st != GPULET_OK) return st;
                 plan.op_bytes = std::max(plan.op_bytes, matmul_workspace(a));
+                s.scratch = true;
             }
         } else {
             return GPULET_EINVAL;
@@ -690,7 +697,7 @@ hipError_t enqueue(const Bound &bd, gpulet_partition *p) {
             e = launch_dwconv(bd.ptr(s.in_buf), s.w, s.b, bd.ptr(s.out_buf), s.N, s.C, s.H, s.W, s.k, s.k2,
                               s.stride, s.pad, s.relu, s.P, s.Q, stream);
         } else if (s.op == GPULET_OP_GROUP_NORM || s.op == GPULET_OP_MATMUL) {
-            // One scratch for all layers: they follow one another on one lane.
+            // One scratch for all layers, which assign_lanes orders.
             int launches = 0;
             e = run_block_layer(bd, s, ctx, stream, &launches);
             if (e != hipSuccess) return e;

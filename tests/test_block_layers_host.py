@@ -1,0 +1,41 @@
+"""Group norm and per-pixel product layers of models without a GPU: what they share, what a run plans and what it refuses."""
+
+import pytest
+
+from paper_2109_01611_amd import gpulet
+
+from test_abi_host import _desc, _layer
+from test_model_lanes_host import _happens_before
+
+W = 1 << 40   # stand-in address, never followed
+
+
+def _conv(i, o):
+    return _layer(op=gpulet.OP_CONV, in_buf=i, out_buf=o, C=16, K=16, R=1, S=1, stride=1, pad=0, w=W)
+
+
+def _norm(i, o, **kw):
+    return _layer(op=gpulet.OP_GROUP_NORM, in_buf=i, out_buf=o, C=16, K=1, eps=1e-5, **kw)
+
+
+def _product(i, o, C=16, K=16, **kw):
+    return _layer(op=gpulet.OP_MATMUL, in_buf=i, out_buf=o, C=C, K=K, w=W, **kw)
+
+
+@pytest.mark.parametrize("kinds", ["nn", "nm", "mn", "mm", "ncn", "nnmm", "mnmn"])
+def test_layers_that_share_scratch_are_ordered_on_two_lanes(kinds):
+    # branches from one tensor, each layer on a buffer of its own: without the scratch nothing would order them
+    make = dict(n=_norm, m=_product, c=_conv)
+    layers = [_conv(0, 2)] + [make[k](2, 3 + i) for i, k in enumerate(kinds)]
+    layers += [_product(3 + i, 3 + len(kinds) + i if i + 1 < len(kinds) else 1) for i in range(len(kinds))]
+    d = _desc(layers, 3 + 2 * len(kinds), (16, 256, 256))
+    assert gpulet.model_workspace_bytes(d, 1) > 0
+    lane, waits = gpulet.model_schedule(d, 1, lanes=2)
+    reach = _happens_before(len(layers), lane, waits)
+    users = [i for i, L in enumerate(layers) if L.op in (gpulet.OP_GROUP_NORM, gpulet.OP_MATMUL)]
+    for a, i in enumerate(users):
+        for j in users[a + 1:]:
+            assert i in reach[j], (i, j, lane, waits)
+    if "c" in kinds:
+        assert set(lane) == {0, 1}       # a convolution beside them still goes where there is room
+    assert gpulet.model_schedule(d, 1, lanes=1) == ([0] * len(layers), [])
