@@ -688,7 +688,9 @@ gpulet_status gpulet_model_buffer_info(const gpulet_model_desc *m, int batch, in
  * (a launch that stands for several layers would store to the output while it
  * still reads the input), and no layer may read what it writes itself; `in` and
  * `out` may not overlap the part of the workspace behind the buffers
- * (GPULET_EINVAL).
+ * (GPULET_EINVAL).  GPULET_EINVAL, before anything is enqueued, also where a
+ * GROUP_NORM or MATMUL layer's tensors are misaligned or overlap in a way that
+ * the layer by itself refuses.
  * If latency_ms is not NULL the call brackets the batch with events, waits
  * for it and stores the elapsed milliseconds; if NULL it returns right after
  * enqueueing.  Counts one batch and `batch` images on the partition.

@@ -520,24 +520,31 @@ bool chain_aligned(const ChainLayer *l, size_t n, const void *x) {
     return true;
 }
 
+// The operands of a GROUP_NORM or MATMUL layer of this run, checked.
+gpulet_status block_args(const Bound &bd, const Step &s, GroupNormArgs &a) {
+    gpulet_group_norm_desc d = s.norm;
+    d.x = bd.ptr(s.in_buf); d.residual = s.res_buf >= 0 ? bd.ptr(s.res_buf) : nullptr; d.y = bd.ptr(s.out_buf);
+    return check_group_norm(&d, a);
+}
+gpulet_status block_args(const Bound &bd, const Step &s, MatmulArgs &a) {
+    gpulet_matmul_desc d = s.mm;
+    d.x = bd.ptr(s.in_buf); d.residual = s.res_buf >= 0 ? bd.ptr(s.res_buf) : nullptr; d.y = bd.ptr(s.out_buf);
+    return check_matmul(&d, a);
+}
+
 // A GROUP_NORM or MATMUL layer.
 hipError_t run_block_layer(const Bound &bd, const Step &s, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
-    const void *x = bd.ptr(s.in_buf), *res = s.res_buf >= 0 ? bd.ptr(s.res_buf) : nullptr;
-    void *y = bd.ptr(s.out_buf), *scratch = bd.plan->op_bytes > 0 ? bd.ws + bd.plan->op_offset : nullptr;
+    void *scratch = bd.plan->op_bytes > 0 ? bd.ws + bd.plan->op_offset : nullptr;
     if (s.op == GPULET_OP_GROUP_NORM) {
-        gpulet_group_norm_desc d = s.norm;
-        d.x = x; d.residual = res; d.y = y;
         GroupNormArgs a;
-        if (check_group_norm(&d, a) != GPULET_OK) return hipErrorInvalidValue;
+        if (block_args(bd, s, a) != GPULET_OK) return hipErrorInvalidValue;
         a.ws = scratch;
         a.ws_bytes = bd.plan->op_bytes;
         if (group_norm_workspace(a) > a.ws_bytes) return hipErrorInvalidValue;
         return launch_group_norm(a, stream, launches);
     }
-    gpulet_matmul_desc d = s.mm;
-    d.x = x; d.residual = res; d.y = y;
     MatmulArgs a;
-    if (check_matmul(&d, a) != GPULET_OK) return hipErrorInvalidValue;
+    if (block_args(bd, s, a) != GPULET_OK) return hipErrorInvalidValue;
     a.ws = scratch;
     a.ws_bytes = bd.plan->op_bytes;
     return launch_matmul(a, ctx, stream, launches);
@@ -726,6 +733,7 @@ hipError_t enqueue(const Bound &bd, gpulet_partition *p) {
     return hipSuccess;
 }
 
+// Before anything is enqueued: a layer that refuses its operands would leave a batch half done.
 gpulet_status check_run_args(const Plan &plan, int batch, const void *in, void *out, void *ws, size_t ws_bytes) {
     if (!in || !out) return GPULET_EINVAL;
     if (plan.ws_bytes > 0) {
@@ -740,6 +748,15 @@ gpulet_status check_run_args(const Plan &plan, int batch, const void *in, void *
             return at < hi && lo < at + plan.bufs[static_cast<size_t>(buf)].bytes_per_image * static_cast<size_t>(batch);
         };
         if (meets(in, plan.in_buf) || meets(out, plan.out_buf)) return GPULET_EINVAL;
+    }
+    const Bound bd{&plan, batch, in, out, static_cast<char *>(ws)};
+    for (const Step &s : plan.steps) {
+        gpulet_status st = GPULET_OK;
+        GroupNormArgs norm;
+        MatmulArgs mm;
+        if (s.op == GPULET_OP_GROUP_NORM) st = block_args(bd, s, norm);
+        else if (s.op == GPULET_OP_MATMUL) st = block_args(bd, s, mm);
+        if (st != GPULET_OK) return st;
     }
     return GPULET_OK;
 }
