@@ -683,14 +683,15 @@ gpulet_status gpulet_model_buffer_info(const gpulet_model_desc *m, int batch, in
  * partition's stream with no host synchronisation in between.  `in` is the
  * input batch (batch*in_H*in_W*in_C bf16), `out` receives the output buffer.
  * `workspace` must be 256-byte aligned device memory of at least
- * gpulet_model_workspace_bytes() bytes (GPULET_ENOMEM otherwise).
+ * gpulet_model_workspace_bytes() bytes (GPULET_ENOMEM otherwise, or, if only
+ * what MATMUL layers would use behind the buffers is missing, slower ones).
  * Where `in`, `out` and `workspace` overlap, every layer is a launch of its own
  * (a launch that stands for several layers would store to the output while it
  * still reads the input), and no layer may read what it writes itself; `in` and
- * `out` may not overlap the part of the workspace behind the buffers
- * (GPULET_EINVAL).  GPULET_EINVAL, before anything is enqueued, also where a
- * GROUP_NORM or MATMUL layer's tensors are misaligned or overlap in a way that
- * the layer by itself refuses.
+ * `out` may not overlap what GROUP_NORM layers use behind the buffers
+ * (GPULET_EINVAL; MATMUL layers do without what they overlap).  GPULET_EINVAL,
+ * before anything is enqueued, also where a GROUP_NORM or MATMUL layer's tensors
+ * are misaligned or overlap in a way that the layer by itself refuses.
  * If latency_ms is not NULL the call brackets the batch with events, waits
  * for it and stores the elapsed milliseconds; if NULL it returns right after
  * enqueueing.  Counts one batch and `batch` images on the partition.

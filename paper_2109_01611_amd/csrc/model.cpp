@@ -59,7 +59,8 @@ struct Plan {
     std::vector<BufState> bufs;
     std::vector<size_t> offset;  // workspace offset per buffer, (size_t)-1 for caller-owned
     size_t ws_bytes = 0;
-    size_t op_offset = 0, op_bytes = 0;  // the end of the workspace: scratch of whichever layer runs
+    size_t op_offset = 0, op_bytes = 0;  // the end of the workspace: scratch of whichever layer runs, and what it cannot do without
+    bool products = false;               // a MATMUL layer, which uses what scratch there is
     int in_buf = 0, out_buf = 0;
 };
 
@@ -201,8 +202,10 @@ void find_chains(Plan &plan) {
 
 size_t round_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
-// Shape inference and validation of a model description for `batch` images.
-gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
+// Shape inference and validation of a model description for `batch` images.  `fastest`: the scratch also holds what MATMUL
+// layers are fastest with on any number of CUs.  Runs leave that out: to look through all numbers takes 7 to 9 us a layer,
+// twice as long as a launch.
+gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan, bool fastest = false) {
     if (!m || !m->layers || m->n_layers < 1 || m->n_bufs < 2 || batch < 1) return GPULET_EINVAL;
     if (m->in_C < 1 || m->in_H < 1 || m->in_W < 1) return GPULET_EINVAL;
     if (m->in_buf < 0 || m->in_buf >= m->n_bufs || m->out_buf < 0 || m->out_buf >= m->n_bufs ||
@@ -357,8 +360,8 @@ gpulet_status build_plan(const gpulet_model_desc *m, int batch, Plan &plan) {
                 MatmulArgs a;
                 const gpulet_status st = check_matmul(&s.mm, a);
                 if (st != GPULET_OK) return st;
-                plan.op_bytes = std::max(plan.op_bytes, matmul_workspace(a));
-                s.scratch = true;
+                if (fastest) plan.op_bytes = std::max(plan.op_bytes, matmul_workspace(a));
+                s.scratch = plan.products = true;
             }
         } else {
             return GPULET_EINVAL;
@@ -470,6 +473,7 @@ struct Bound {
     const void *in;
     void *out;
     char *ws;
+    size_t op_bytes;   // scratch behind the buffers
     void *ptr(int buf) const {
         if (buf == plan->in_buf) return const_cast<void *>(in);
         if (buf == plan->out_buf) return out;
@@ -534,19 +538,19 @@ gpulet_status block_args(const Bound &bd, const Step &s, MatmulArgs &a) {
 
 // A GROUP_NORM or MATMUL layer.
 hipError_t run_block_layer(const Bound &bd, const Step &s, const LaunchCtx &ctx, hipStream_t stream, int *launches) {
-    void *scratch = bd.plan->op_bytes > 0 ? bd.ws + bd.plan->op_offset : nullptr;
+    void *scratch = bd.op_bytes > 0 ? bd.ws + bd.plan->op_offset : nullptr;
     if (s.op == GPULET_OP_GROUP_NORM) {
         GroupNormArgs a;
         if (block_args(bd, s, a) != GPULET_OK) return hipErrorInvalidValue;
         a.ws = scratch;
-        a.ws_bytes = bd.plan->op_bytes;
+        a.ws_bytes = bd.op_bytes;
         if (group_norm_workspace(a) > a.ws_bytes) return hipErrorInvalidValue;
         return launch_group_norm(a, stream, launches);
     }
     MatmulArgs a;
     if (block_args(bd, s, a) != GPULET_OK) return hipErrorInvalidValue;
     a.ws = scratch;
-    a.ws_bytes = bd.plan->op_bytes;
+    a.ws_bytes = bd.op_bytes;
     return launch_matmul(a, ctx, stream, launches);
 }
 
@@ -733,23 +737,29 @@ hipError_t enqueue(const Bound &bd, gpulet_partition *p) {
     return hipSuccess;
 }
 
-// Before anything is enqueued: a layer that refuses its operands would leave a batch half done.
-gpulet_status check_run_args(const Plan &plan, int batch, const void *in, void *out, void *ws, size_t ws_bytes) {
+// What a run works on, checked before anything is enqueued: a layer that refuses its operands would leave a batch half done.
+gpulet_status bind(const Plan &plan, int batch, const void *in, void *out, void *ws, size_t ws_bytes, Bound &bd) {
     if (!in || !out) return GPULET_EINVAL;
     if (plan.ws_bytes > 0) {
         if (!ws) return GPULET_EINVAL;
         if (ws_bytes < plan.ws_bytes) return GPULET_ENOMEM;
         if (reinterpret_cast<uintptr_t>(ws) % kAlign != 0) return GPULET_EINVAL;
     }
-    if (plan.op_bytes > 0) {
-        const uintptr_t lo = reinterpret_cast<uintptr_t>(ws) + plan.op_offset, hi = lo + plan.op_bytes;
-        auto meets = [&](const void *p, int buf) {
+    bd = Bound{&plan, batch, in, out, static_cast<char *>(ws), 0};
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(ws) + plan.op_offset;
+    if (plan.op_bytes > 0 || (plan.products && ws && lo % kAlign == 0 && ws_bytes > plan.op_offset)) {
+        // scratch is what lies behind the buffers and in front of an input or output that lies there too
+        uintptr_t hi = reinterpret_cast<uintptr_t>(ws) + ws_bytes;
+        auto leave = [&](const void *p, int buf) {
             const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-            return at < hi && lo < at + plan.bufs[static_cast<size_t>(buf)].bytes_per_image * static_cast<size_t>(batch);
+            if (at < hi && lo < at + plan.bufs[static_cast<size_t>(buf)].bytes_per_image * static_cast<size_t>(batch))
+                hi = std::max(at, lo);
         };
-        if (meets(in, plan.in_buf) || meets(out, plan.out_buf)) return GPULET_EINVAL;
+        leave(in, plan.in_buf);
+        leave(out, plan.out_buf);
+        bd.op_bytes = hi - lo;
+        if (bd.op_bytes < plan.op_bytes) return GPULET_EINVAL;
     }
-    const Bound bd{&plan, batch, in, out, static_cast<char *>(ws)};
     for (const Step &s : plan.steps) {
         gpulet_status st = GPULET_OK;
         GroupNormArgs norm;
@@ -832,7 +842,7 @@ extern "C" gpulet_status gpulet_model_workspace_bytes(const gpulet_model_desc *m
                                                       size_t *bytes) {
     if (!bytes) return GPULET_EINVAL;
     Plan plan;
-    gpulet_status st = build_plan(m, batch, plan);
+    gpulet_status st = build_plan(m, batch, plan, true);
     if (st != GPULET_OK) return st;
     *bytes = plan.ws_bytes;
     return GPULET_OK;
@@ -862,9 +872,9 @@ extern "C" gpulet_status gpulet_run_model(const gpulet_model_desc *m, int batch,
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, batch, in, out, workspace, workspace_bytes);
+    Bound bd;
+    st = bind(plan, batch, in, out, workspace, workspace_bytes, bd);
     if (st != GPULET_OK) return st;
-    const Bound bd{&plan, batch, in, out, static_cast<char *>(workspace)};
     if (latency_ms) {
         EventPair ev;
         GPULET_HIP(ev.create());
@@ -887,9 +897,9 @@ extern "C" gpulet_status gpulet_profile_model(const gpulet_model_desc *m, int ba
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, batch, in, out, workspace, workspace_bytes);
+    Bound bd;
+    st = bind(plan, batch, in, out, workspace, workspace_bytes, bd);
     if (st != GPULET_OK) return st;
-    const Bound bd{&plan, batch, in, out, static_cast<char *>(workspace)};
 
     for (int i = 0; i < warmup; ++i) {
         GPULET_HIP(enqueue(bd, p));
@@ -976,9 +986,9 @@ extern "C" gpulet_status gpulet_model_graph_create(const gpulet_model_desc *m, i
     Plan plan;
     gpulet_status st = build_plan(m, batch, plan);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan, batch, in, out_buf, workspace, workspace_bytes);
+    Bound bd;
+    st = bind(plan, batch, in, out_buf, workspace, workspace_bytes, bd);
     if (st != GPULET_OK) return st;
-    const Bound bd{&plan, batch, in, out_buf, static_cast<char *>(workspace)};
     GPULET_HIP(hipStreamSynchronize(p->stream));
     hipGraph_t graph = nullptr;
     hipGraphExec_t exec = nullptr;
@@ -1114,13 +1124,14 @@ extern "C" gpulet_status gpulet_profile_corun(
     if (st != GPULET_OK) return st;
     st = build_plan(mb, batch_b, plan_b);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan_a, batch_a, in_a, out_a, ws_a, ws_a_bytes);
+    Bound bound_a, bound_b;
+    st = bind(plan_a, batch_a, in_a, out_a, ws_a, ws_a_bytes, bound_a);
     if (st != GPULET_OK) return st;
-    st = check_run_args(plan_b, batch_b, in_b, out_b, ws_b, ws_b_bytes);
+    st = bind(plan_b, batch_b, in_b, out_b, ws_b, ws_b_bytes, bound_b);
     if (st != GPULET_OK) return st;
 
-    CorunSide sa{&plan_a, Bound{&plan_a, batch_a, in_a, out_a, static_cast<char *>(ws_a)}, pa, batch_a, warmup, cap_a, lat_a};
-    CorunSide sb{&plan_b, Bound{&plan_b, batch_b, in_b, out_b, static_cast<char *>(ws_b)}, pb, batch_b, warmup, cap_b, lat_b};
+    CorunSide sa{&plan_a, bound_a, pa, batch_a, warmup, cap_a, lat_a};
+    CorunSide sb{&plan_b, bound_b, pb, batch_b, warmup, cap_b, lat_b};
     std::atomic<int> ready{0}, done_a{0}, done_b{0};
     std::thread ta(corun_thread, &sa, &ready, window_ms, &done_a, &done_b);
     std::thread tb(corun_thread, &sb, &ready, window_ms, &done_b, &done_a);

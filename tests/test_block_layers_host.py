@@ -1,5 +1,7 @@
 """Group norm and per-pixel product layers of models without a GPU: what they share, what a run plans and what it refuses."""
 
+import time
+
 import pytest
 
 from paper_2109_01611_amd import gpulet
@@ -39,3 +41,32 @@ def test_layers_that_share_scratch_are_ordered_on_two_lanes(kinds):
     if "c" in kinds:
         assert set(lane) == {0, 1}       # a convolution beside them still goes where there is room
     assert gpulet.model_schedule(d, 1, lanes=1) == ([0] * len(layers), [])
+
+
+def _seconds(f, n=30):
+    best = 1.0
+    for _ in range(n):
+        t = time.perf_counter()
+        f()
+        best = min(best, time.perf_counter() - t)
+    return best
+
+
+def test_a_run_does_not_look_through_all_numbers_of_cus():
+    # What a run plans (also for the shape of a buffer) against what the size of the workspace takes, which looks for every
+    # product through 32 numbers of CUs: before runs left that out, the two took the same time.
+    n = 24
+    layers = [_product(0 if i == 0 else 1 + i, 2 + i if i + 1 < n else 1, 256, 256) for i in range(n)]
+    d = _desc(layers, n + 1, (256, 24, 24))
+    run = _seconds(lambda: gpulet.model_buffer_info(d, 2, 1))
+    size = _seconds(lambda: gpulet.model_workspace_bytes(d, 2))
+    assert run < 0.5 * size, (run, size)
+
+
+def test_workspace_still_holds_what_products_are_fastest_with():
+    # 4096 x 4096 pixels' products of a depth that is no multiple of 8: copies of both operands
+    mm = gpulet.matmul_desc(1 << 41, 1 << 42, None, 1 << 43, 64 * 64, 4096, 1022)
+    need = gpulet.matmul_workspace_bytes(mm)
+    assert need > 0
+    d = _desc([_product(0, 1, 1022, 4096)], 2, (1022, 64, 64))
+    assert gpulet.model_workspace_bytes(d, 1) == (need + 255) // 256 * 256

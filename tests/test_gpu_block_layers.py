@@ -46,3 +46,47 @@ def test_a_layer_that_refuses_its_tensors_refuses_the_run(kind):
         g = x.double().view(64, 4, 4)
         want = (g - g.mean((0, 2), keepdim=True)) / torch.sqrt(g.var((0, 2), unbiased=False, keepdim=True) + 1e-5)
         assert bool(((y.double().view(64, 4, 4) - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all())
+
+
+def test_products_use_what_scratch_there_is_and_no_more():
+    # 4096 pixels of 1022 channels: both operands are laid out anew where there is room.  Small integers: sums are exact.
+    C, K, H = 1022, 1024, 64
+    g = torch.Generator().manual_seed(1)
+    x = torch.randint(-4, 5, (H * H, C), generator=g).to(DEV).bfloat16()
+    w = torch.randint(-4, 5, (K, C), generator=g).to(DEV).bfloat16()
+    want = x.float() @ w.float().t()
+    d = _desc([_layer(op=gpulet.OP_MATMUL, in_buf=0, out_buf=1, C=C, K=K, out_fp32=1, w=w.data_ptr())], 2, (C, H, H))
+    n = gpulet.model_workspace_bytes(d, 1)
+    assert n > 0
+    y = torch.empty(H * H, K, device=DEV)
+    arena = torch.empty(2 * n + y.numel() * 4 + 4096, dtype=torch.uint8, device=DEV)
+    with gpulet.Partition(0, 100, 0) as part:
+        def run(out, ws, size):
+            arena.fill_(0xFF)
+            y.fill_(-1.0)
+            torch.cuda.synchronize()
+            gpulet.run_model(d, 1, part, x, out, ws, size)
+            part.sync()
+            launched = part.kernel_launches()
+            return launched
+        before = part.kernel_launches()
+        for size, launches in ((n, 2), (2 * n, 2), (n // 2 // 256 * 256, 1), (0, 1)):
+            now = run(y, arena if size else None, size)
+            assert torch.equal(y, want) and now - before == launches, size
+            assert bool((arena[n:] == 0xFF).all())          # nothing behind what the model asks for
+            before = now
+        # the output inside of the scratch, at its start and further back
+        for at, launches in ((0, 1), (512, 1), (n, 2)):
+            out = arena[at:at + y.numel() * 4].view(torch.float32).view(H * H, K)
+            now = run(out, arena, arena.numel() // 256 * 256)
+            assert torch.equal(out, want) and now - before == launches, at
+            before = now
+        graph_ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV)
+        graph = gpulet.ModelGraph(d, 1, part, x, y, graph_ws, n)
+        for _ in range(3):
+            y.fill_(-1.0)
+            torch.cuda.synchronize()
+            graph.launch()
+            part.sync()
+            assert torch.equal(y, want)
+        graph.destroy()
