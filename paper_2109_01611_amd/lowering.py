@@ -93,10 +93,10 @@ class DeviceModel:
         self.in_shape = tuple(model.in_shape)
         self._keep = []  # device tensors the layer records point into
         nodes = [nd for nd in model.nodes]
-        # channel padding of the model input (only convolutions may read it then)
+        # channel padding of the model input (only convolutions may read it then, and not as a residual)
         c_in = model.in_shape[0]
-        readers = [nd for nd in nodes if nd.src == "x"]
-        if not all(nd.op == "conv" for nd in readers):
+        readers = [nd for nd in nodes if "x" in _reads(nd)]
+        if not all(nd.op == "conv" and nd.attr["residual"] != "x" for nd in readers):
             self.in_pad = 0
         elif c_in <= 4 and all(nd.attr["k"] in (3, 5, 7) and nd.attr["K"] % 8 == 0 for nd in readers):
             self.in_pad = 4 - c_in

@@ -4,7 +4,7 @@ import time
 
 import pytest
 
-from paper_2109_01611_amd import gpulet
+from paper_2109_01611_amd import gpulet, lowering, workloads
 
 from test_abi_host import _desc, _layer
 from test_model_lanes_host import _happens_before
@@ -70,3 +70,21 @@ def test_workspace_still_holds_what_products_are_fastest_with():
     assert need > 0
     d = _desc([_product(0, 1, 1022, 4096)], 2, (1022, 64, 64))
     assert gpulet.model_workspace_bytes(d, 1) == (need + 255) // 256 * 256
+
+
+def _reads_its_input_again():
+    n = workloads
+    nodes = [n._conv("a", "x", "a", 3, 16, 3, 1, 1, False), n._groupnorm("g", "a", "b", 16, 4, "silu"),
+             n._matmul("m", "b", "c", 16, 3, residual="x"), n._groupnorm("h", "c", "d", 3, 1, residual="x"),
+             n._conv("e", "x", "e", 3, 8, 3, 1, 1, False), n._conv("f", "d", "y", 3, 8, 3, 1, 1, True, residual="e")]
+    return n.Model("input_again", (3, 10, 10), "normal", nodes, "y")
+
+
+def test_the_models_input_as_a_residual_is_not_padded():
+    # convolutions of the input get zero channels, which a residual of three channels has not
+    model = _reads_its_input_again()
+    dm = lowering.DeviceModel(model, workloads.parameters(model, 0), "cpu")
+    assert dm.in_pad == 0 and gpulet.model_workspace_bytes(dm.desc, 2) > 0
+    plain = model._replace(nodes=[nd._replace(attr=dict(nd.attr, residual=None)) if nd.attr.get("residual") == "x" else nd
+                                  for nd in model.nodes])
+    assert lowering.DeviceModel(plain, workloads.parameters(plain, 0), "cpu").in_pad == 1

@@ -3,9 +3,12 @@
 import pytest
 import torch
 
-from paper_2109_01611_amd import gpulet
+import oracle
+from paper_2109_01611_amd import gpulet, lowering, workloads
 
+from gpu_util import MODEL_TOL
 from test_abi_host import _desc, _layer
+from test_block_layers_host import _reads_its_input_again
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -90,3 +93,13 @@ def test_products_use_what_scratch_there_is_and_no_more():
             part.sync()
             assert torch.equal(y, want)
         graph.destroy()
+
+
+def test_a_model_that_reads_its_input_again():
+    model = _reads_its_input_again()
+    params, x = workloads.parameters(model, 3), workloads.batch_input(model, 3, 3)
+    dm = lowering.DeviceModel(model, params, DEV)
+    with gpulet.Partition(0, 100, 0) as part:
+        y, _ = dm.run(part, dm.input_to_device(x))
+    want = oracle.run_model(model, params, x)
+    assert max(oracle.rel_err(lowering.nhwc_to_nchw(y), want)) <= MODEL_TOL
