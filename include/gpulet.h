@@ -545,7 +545,9 @@ gpulet_status gpulet_matmul(const gpulet_matmul_desc *d, void *workspace, size_t
  * may share no element with x, residual, gamma or beta.
  * Errors: GPULET_EINVAL for a NULL descriptor, x or y; non-positive sizes; groups
  * that do not divide C; a ch_stride below C; an image of 2^31 bytes or more
- * (counting the stored pixels); more than 2^21 (image, group) pairs; a negative,
+ * (counting the stored pixels); more than 2^21 (image, group) pairs; more than
+ * 2^32 threads (maps of 4 GiB may, if they have few pixels and rows that start
+ * anywhere; ordinary ones from 128 GiB on); a negative,
  * infinite or NaN eps; an unknown type or activation; misaligned pointers and
  * overlap as gpulet_matmul.  GPULET_ENOMEM when workspace_bytes is less than
  * gpulet_group_norm_workspace_bytes says.

@@ -171,6 +171,7 @@ struct GroupNormArgs {
     size_t ws_bytes;
 };
 gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a);
+bool group_norm_fits(const GroupNormArgs &a);           // whether its launches may have as many threads
 size_t group_norm_workspace(const GroupNormArgs &a);   // bytes launch_group_norm needs
 hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream, int *launches = nullptr);
 

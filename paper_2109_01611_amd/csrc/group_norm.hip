@@ -511,13 +511,17 @@ constexpr size_t kStreamBytes = 64 << 20;
 struct Plan {
     enum Form { HELD, TWO } form;
     int V, iters;
-    bool stream_out;
+    bool stream_out, fits;
     Params p, q;   // of the only or first launch, and of the second
 };
 
-void set_blocks(Params &p, int N, int per_image) {
-    p.total = N * per_image;
-    p.per_die = (p.total + 7) / 8;
+// -> whether a launch may have as many threads: fewer than 2^32.
+bool set_blocks(Params &p, int N, long long per_image) {
+    const long long total = N * per_image, per_die = (total + 7) / 8;
+    if (8 * per_die * p.threads >= (1LL << 32)) return false;
+    p.total = static_cast<int>(total);
+    p.per_die = static_cast<int>(per_die);
+    return true;
 }
 
 void set_units(Params &p, int V, int gb, int slices, int threads) {
@@ -539,14 +543,14 @@ void set_units(Params &p, int V, int gb, int slices, int threads) {
 }
 
 // Chunks of about `piece` bytes, made of whole batches.
-void set_chunks(Params &p, int V, int unit_bytes, int gb, int slices, int threads, size_t block_bytes, size_t piece, int N) {
+bool set_chunks(Params &p, int V, int unit_bytes, int gb, int slices, int threads, size_t block_bytes, size_t piece, int N) {
     set_units(p, V, gb, slices, threads);
     const int chunks = static_cast<int>(std::max<size_t>(1, block_bytes / piece));
     const int whole = p.R * batch_of(unit_bytes);
     p.chunk = ((p.HW + chunks - 1) / chunks + whole - 1) / whole * whole;
     p.chunks = (p.HW + p.chunk - 1) / p.chunk;
     p.d_chunks = make_fastdiv(p.chunks);
-    set_blocks(p, N, p.n_cb * p.chunks);
+    return set_blocks(p, N, 1LL * p.n_cb * p.chunks);
 }
 
 Plan make_plan(const GroupNormArgs &a) {
@@ -584,7 +588,7 @@ Plan make_plan(const GroupNormArgs &a) {
             pl.form = Plan::HELD;
             pl.iters = p.iters = iters;
             set_units(p, V, gb, 1, threads);
-            set_blocks(p, a.N, p.n_cb);
+            pl.fits = set_blocks(p, a.N, p.n_cb);
             return pl;
         }
     }
@@ -605,8 +609,8 @@ Plan make_plan(const GroupNormArgs &a) {
     pl.stream_out = static_cast<size_t>(a.N) * p.HW * p.C * es >= kStreamBytes;
     pl.q = p;
     const int fewest = ((gb * p.cg / V + slices - 1) / slices + 63) / 64 * 64;   // threads of one row
-    set_chunks(p, V, V * es, gb, slices, std::max(stats >= (64 << 10) ? 512 : 256, fewest), block_bytes, stats, a.N);
-    set_chunks(pl.q, V, V * es, gb, slices, std::max(256, fewest), block_bytes, apply, a.N);
+    pl.fits = set_chunks(p, V, V * es, gb, slices, std::max(stats >= (64 << 10) ? 512 : 256, fewest), block_bytes, stats, a.N);
+    pl.fits = set_chunks(pl.q, V, V * es, gb, slices, std::max(256, fewest), block_bytes, apply, a.N) && pl.fits;
     pl.q.stat_chunks = p.chunks;
     pl.q.stat_chunk = p.chunk;
     return pl;
@@ -666,6 +670,8 @@ hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t stream, int *la
     if (a.dtype == GPULET_F16) return launch_act<_Float16>(pl, stream);
     return launch_act<float>(pl, stream);
 }
+
+bool group_norm_fits(const GroupNormArgs &a) { return make_plan(a).fits; }
 
 size_t group_norm_workspace(const GroupNormArgs &a) {
     const Plan pl = make_plan(a);

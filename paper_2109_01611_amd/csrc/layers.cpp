@@ -104,6 +104,8 @@ gpulet_status check_group_norm(const gpulet_group_norm_desc *d, GroupNormArgs &a
     if (!(a.x == a.y && a.ldx == a.ldy) && meet(y, make_rows(a.x, all, es * C, 1ull * es * a.ldx))) return GPULET_EINVAL;
     if (!(a.residual == a.y && a.ldr == a.ldy) && meet(y, make_rows(a.residual, all, es * C, 1ull * es * a.ldr)))
         return GPULET_EINVAL;
+    // a thread has nearly an element at least
+    if (all * C > (1ull << 30) && !group_norm_fits(a)) return GPULET_EINVAL;
     return GPULET_OK;
 }
 
