@@ -96,3 +96,12 @@ def test_first_values_far_from_the_others(size):
             c.x.copy_(px.view(N, H, W, C))
             c.run()
             _close(c, (every, first, step))
+
+
+@pytest.mark.parametrize("size", FORMS[:3], ids=str)
+def test_large_means(size):
+    # bounds that, at a mean of 1000, an fp32 mean(x^2) - mean^2 does not meet (test_group_norm_ends_host.py)
+    for dtype, mean in (("f32", 1000.0), ("f32", -30.0), ("f16", 100.0)):
+        c = Case(5, *size, dtype=dtype, mean=mean)
+        c.run()
+        _close(c, (dtype, mean))
