@@ -470,7 +470,8 @@ enum { GPULET_BF16 = 0, GPULET_F16 = 1, GPULET_F32 = 2 };
 /* Activations of the layers below, on the fp32 value before it is rounded:
  *   RELU max(v, 0) (NaN stays NaN)      SILU v / (1 + exp(-v))
  *   GELU v * Phi(v), Phi the normal distribution function
- *   GELU_TANH v / 2 * (1 + tanh(sqrt(2 / pi) * (v + 0.044715 v^3))) */
+ *   GELU_TANH v / 2 * (1 + tanh(sqrt(2 / pi) * (v + 0.044715 v^3)))
+ * Minus infinity gives 0 by RELU and NaN (infinity times 0) by the last three. */
 enum { GPULET_ACT_NONE = 0, GPULET_ACT_RELU = 1, GPULET_ACT_SILU = 2, GPULET_ACT_GELU = 3, GPULET_ACT_GELU_TANH = 4 };
 
 /*

@@ -105,3 +105,23 @@ def test_large_means(size):
         c = Case(5, *size, dtype=dtype, mean=mean)
         c.run()
         _close(c, (dtype, mean))
+
+
+def test_two_at_once_on_two_streams():
+    cs = [Case(11 + i, *size, act="silu", res=True) for i, size in enumerate([(3, 64, 64, 320, 32), (2, 200, 200, 64, 4)])]
+    want = [c.run().clone() for c in cs]
+    descs = [c.desc() for c in cs]
+    sizes = [gpulet.group_norm_workspace_bytes(d) for d in descs]
+    assert min(sizes) > 0
+    spaces = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) for n in sizes]
+    streams = [torch.cuda.Stream() for _ in cs]
+    for c in cs:
+        c.y.fill_(GUARD)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, d, ws, n in zip(streams, descs, spaces, sizes):
+            gpulet.group_norm(d, ws, n, st.cuda_stream)
+    torch.cuda.synchronize()
+    for c, w in zip(cs, want):
+        assert torch.equal(c.y, w)
+        c.check_guards()
