@@ -22,6 +22,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "act_device.h"
 #include "device_util.h"
@@ -203,9 +204,10 @@ __device__ __forceinline__ typename RawUnit<V * sizeof(T)>::Type finish_unit(con
     return pack<T, V>(f);
 }
 
-// Held: gb groups of one image in the registers of a workgroup, NR units a thread.
+// Held: gb groups of one image in the registers of a workgroup, NR units a thread.  Two units of 8 channels take 66 registers
+// if they may; with 64 a second workgroup of 1024 threads has room on a CU (32 images of 16x16x1280 22 us instead of 28).
 template <typename T, int V, int NR, ActCode A>
-__global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
+__global__ __launch_bounds__(kMaxThreads, V == 8 && NR == 2 ? 8 : 4) void held_kernel(Params p) {
     constexpr int UB = V * static_cast<int>(sizeof(T));
     typedef typename RawUnit<UB>::Type Raw;
     constexpr bool EARLY_RES = NR * UB <= 64;   // the residual, too, is requested before the statistics
@@ -271,14 +273,13 @@ __global__ __launch_bounds__(kMaxThreads) void held_kernel(Params p) {
     units([&](int i) {
         float f[V];
         unpack<T, V>(xv[i], f);
-        float t = 0.f, q = 0.f;
+        const float from = valid(i) ? near : 0.f;   // units left out were loaded as zeros
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            t += f[j] - near;
-            q += (f[j] - near) * (f[j] - near);
+            const float e = f[j] - from;
+            d[0] += e;
+            d[1] += e * e;
         }
-        d[0] += valid(i) ? t : 0.f;
-        d[1] += valid(i) ? q : 0.f;
     });
     group_sums(d, p, at.group, reinterpret_cast<float(*)[2]>(part), res2);
     const float more = d[0] * inv, mean = near + more;
@@ -356,9 +357,10 @@ struct Walk {
 
 // Statistics of one chunk of an image for the groups of a workgroup.  A thread sums the differences of a batch from the mean
 // of what it summed before, and their squares, and joins the batch's statistics to those before; the first batch's are
-// from its own mean.  The roundings of the squares' sum are at most B V 2^-24 of it, and of the n0 + nb differences
-// joined so far, the nb new ones, whose mean is D away, add n0 nb / (n0 + nb) D^2, at least half of what their
-// squares' sum has from D: the roundings are no more than 2 B V 2^-24 (4e-6) of the result, wherever the values lie.
+// from the mean of a quarter of its values, at least.  The roundings of the squares' sum are at most B V 2^-24 of it.  Of the
+// n0 + nb values joined so far, the nb new ones, whose mean is D away, add n0 nb / (n0 + nb) D^2, at least half of what their
+// squares' sum has from D; the first batch's sum is at most four times what it is from the batch's own mean.  So the roundings
+// are no more than 4 B V 2^-24 (8e-6) of the result, wherever the values lie.
 // (One sum of differences from the thread's first value: up to 1e-2 of it where that value is the only one that lies far off.)
 template <typename T, int V>
 __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
@@ -375,8 +377,8 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
     W w(p, at, q0, q1);
     typename W::Raw xv[W::B];
     w.load(xs, p.ldx, xv);
-    // Calls f with every value of a batch, or with `none` for one that is not there.  -> how many are there
-    auto each = [&](const typename W::Raw (&raw)[W::B], bool whole, float none, auto &&f) {
+    // Calls f with the first N values of every unit of a batch, or with `none` for one that is not there.  -> how many are there
+    auto each = [&](const typename W::Raw (&raw)[W::B], bool whole, float none, auto N, auto &&f) {
         int units = whole && at.in ? W::B : 0;
 #pragma unroll
         for (int i = 0; i < W::B; ++i) {
@@ -385,14 +387,16 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
             float v[V];
             unpack<T, V>(raw[i], v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) f(ok ? v[j] : none);
+            for (int j = 0; j < N; ++j) f(ok ? v[j] : none);
         }
-        return static_cast<float>(units * V);
+        return static_cast<float>(units * N);
     };
+    constexpr std::integral_constant<int, V> ALL{};
+    constexpr std::integral_constant<int, V < 2 ? V : 2> SOME{};
     float first[V];
     unpack<T, V>(xv[0], first);
     float sum = 0.f;
-    float nb = each(xv, w.full(), first[0], [&](float v) { sum += v - first[0]; });
+    float nb = each(xv, w.full(), first[0], SOME, [&](float v) { sum += v - first[0]; });
     // of equal values the mean is that value, to the bit; of none it is zero
     Stat all{0.f, first[0] + sum * __builtin_amdgcn_rcpf(fmaxf(nb, 1.f)), 0.f};
     while (true) {
@@ -405,7 +409,7 @@ __global__ __launch_bounds__(kMaxThreads) void stats_kernel(Params p) {
         if (more) next.load(xs, p.ldx, xv);   // on its way while the batch before is summed
         float sq = 0.f;
         sum = 0.f;
-        nb = each(cur, w.full(), all.mean, [&](float v) {
+        nb = each(cur, w.full(), all.mean, ALL, [&](float v) {
             const float d = v - all.mean;
             sum += d;
             sq += d * d;
