@@ -8,7 +8,7 @@
 // * held: a workgroup keeps whole groups of one image in registers: one launch, x read once.  For up to kHeldBytes.
 // * two launches for larger groups: the first reduces chunks of an image to (mean, sum of squared differences) per group,
 //   the second joins them and reads x again, from the last-level cache where x fits there.  8 maps of 256x256x128 (134 MB)
-//   take 22 + 42 us, as much as 4.2 TB/s of the 268 MB that have to move; a copy of that size reaches 5.1.
+//   take 21 + 42 us, as much as 4.3 TB/s of the 268 MB that have to move; a copy of that size reaches 5.1.
 //
 // A single launch that holds what it read while all workgroups of an image exchange their sums would have to wait for
 // workgroups that may not be running: another launch of the same kind on another stream could hold their places.
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kMaxThreads, V == 8 && NR == 2 ? 8 : 4) void held_k
     auto base = [&](int ld) { return static_cast<unsigned>(at.row * ld + at.c) * static_cast<unsigned>(sizeof(T)); };
     auto step = [&](int i, int ld) { return static_cast<unsigned>(min(i, full) * p.R * ld) * static_cast<unsigned>(sizeof(T)); };
     // For every register with a unit.  Where a thread has many, those without one are left out four at a time (7 images of
-    // 11 x 18 x 96 in 32 groups, 10 units of 24: 7.4 us, computed for nothing 11.9); a test in front of few costs 3 %.
+    // 11 x 18 x 96 in 32 groups, 10 units of 24: 7.3 us, computed for nothing 11.9); a test in front of few costs 3 %.
     auto units = [&](auto &&f) {
 #pragma unroll
         for (int i0 = 0; i0 < NR; i0 += 4) {
@@ -314,8 +314,8 @@ __device__ __forceinline__ Stat join_lanes(Stat s, int lanes) {
     return s;
 }
 
-// Units in flight a thread in the two launches.  Twice as many are no faster (apply kernel of 5 images of 37 x 29 x 246 fp32
-// 4.6 us instead of 4.3) and make longer code.
+// Units in flight a thread in the two launches.  Twice as many are no faster (5 images of 37 x 29 x 246 fp32 10.2 us instead
+// of 9.2) and make longer code.
 constexpr int batch_of(int unit_bytes) { return unit_bytes >= 8 ? 4 : 8; }
 
 // A thread's walk over the pixels of a chunk, batch_of(UB) units at a time: `full` batches without a test, then one with.
@@ -497,12 +497,12 @@ __global__ __launch_bounds__(kMaxThreads) void apply_kernel(Params p) {
 // ---- host side
 
 // Bytes of the groups a workgroup holds, at most.  Above, too few workgroups read pieces of pixels too short for the memory
-// system: held and in two launches took, bf16, 32 groups,
-//    5 KB  8x8x1280   1 image  4.3 and 7.7 us    32 images  7.8 and 10.5
-//   12 KB  14x14x1024 1 image  4.6 and 7.4       32 images 11.1 and 15.3
-//   20 KB  16x16x1280 1 image  7.5 and 7.6       32 images 21.6 and 21.0
-//   49 KB  28x28x256  1 image 11.0 and 7.5       32 images 13.5 and 15.0
-//   80 KB  32x32x1280 1 image 11.8 and 8.2       32 images 62   and 51
+// system: held and in two launches took, bf16, 32 groups, in a graph,
+//    5 KB  8x8x1280   1 image  4.3 and 7.7 us    32 images  7.7 and 10.6
+//   12 KB  14x14x1024 1 image  4.6 and 7.4       32 images 10.6 and 14.6
+//   20 KB  16x16x1280 1 image  7.6 and 7.7       32 images 21.8 and 20.7
+//   49 KB  28x28x256  1 image 10.4 and 7.5       32 images 13.1 and 14.4
+//   80 KB  32x32x1280 1 image 11.5 and 8.2       32 images 51.6 and 54.4
 constexpr size_t kHeldBytes = 32 << 10;
 constexpr int kHeldDwords = 24;           // registers of a thread that hold units
 // Bytes of a workgroup's chunk.  Statistics: 32 chunks (one for each lane that joins them), unless they are out of these

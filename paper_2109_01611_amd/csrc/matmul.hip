@@ -3,20 +3,21 @@
 // for the per-pixel and per-row layers of a forward pass (paper Sec. 5) that a ReLU convolution or the fully connected
 // layer cannot stand for: wide activations, fp16, fp32 results, rows that are slices of wider ones, any number of rows.
 //
-// Forms, chosen per call by an estimate of their times (choose_matmul):
+// Forms, chosen per call by an estimate of their times (choose_matmul).  Times are those of a call in a graph of 20.
 //   ring     up to 64x64 of y a workgroup, whose wavefronts share the depth, each with slices of its own in LDS and no barrier
-//            before the end.  Few rows, few tiles.  Bound by memory: 1 x 4096 x 4096 7.5 us (4.5 TB/s of the weights),
-//            24 x 1024 x 4096 4.9, 197 x 1024 x 4096 8.7.
+//            before the end.  Few rows, few tiles.  Bound by memory: 1 x 4096 x 4096 5.3 us (6.3 TB/s of the weights, part of
+//            which are in the last-level cache), 24 x 1024 x 4096 4.7, 197 x 1024 x 4096 7.9.
 //   tile     64x64, 128x64 and 128x128 tiles that a workgroup goes through slice by slice.  Bound by the rate at which a CU
-//            takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128 56 us, 933 TFLOP/s.
+//            takes operands (60 to 85 KB/us, whatever lies in flight): 6272 x 1024 x 4096 in 128x128 58 to 64 us, 820 to
+//            900 TFLOP/s.
 //            The 64x64 one also with a depth that up to eight workgroups share, whose sums meet in the workspace: tall y with
-//            few tiles and a long depth (1742 x 216 x 3816 15.7 us, in rings 20.3).
+//            few tiles and a long depth (1742 x 216 x 3816 15.0 us, in rings 19.2).
 //   big      256x256 tiles, 160 KB of LDS: as many matrix instructions as transfers can feed.  8192 x 4096 x 4096 216 us,
-//            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 1.33.
+//            1.27 PFLOP/s (1.25 for the library's product of that size); 8192^3 820 us, 1.34.
 //   direct,  rows that do not start at multiples of 16 bytes or a depth that is not a multiple of 8: operands go from memory
 //   staged   into the matrix instructions (few rows, few tiles), or through registers into LDS (64x64 tiles).
-//            200 x 300 x 4001 9.6 us.  Larger products of such operands lay them out anew in the workspace first and
-//            take the forms above: 2048 x 1024 x 1001 16.3 us (staged 22.5), 4096 x 4096 x 1022 46 (84).
+//            200 x 300 x 4001 8.5 us.  Larger products of such operands lay them out anew in the workspace first and
+//            take the forms above: 2048 x 1024 x 1001 18.2 us (staged 21.6), 4096 x 4096 x 1022 45 (84).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -861,8 +862,8 @@ __global__ __launch_bounds__(256) void join_kernel(Params p) {
 
 // ---- host side
 
-// Microseconds of the forms, fitted to 130 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192 (what is
-// chosen takes 3 % longer than the fastest form, geometric mean).  A CU takes its share of the workgroups in rounds of
+// Microseconds of the forms, fitted on 256 CUs to 130 shapes of 1 to 8192 rows, 32 to 8192 columns and depths of 64 to 8192
+// (what is chosen takes 3 % longer than the fastest form, geometric mean).  A CU takes its share of the workgroups in rounds of
 // `resident`; a round costs `round`.  A slice of a tile takes `near` + `far` * (how much of 8 MB the operands are: from the
 // caches or from memory) when it has the CU for itself, and `busy` times the workgroups that share the CU if that is longer.
 // `finish`: the epilogue of a workgroup.
@@ -889,7 +890,8 @@ constexpr double kJoin = 2.5, kJoinMb = 0.34;
 constexpr int kMaxSplit = 8;
 // The launch that lays rows out anew, likewise.
 constexpr double kPack = 4.5, kPackMb = 0.3;
-// What a call of more than one launch takes the host, and each launch of it: a shorter call waits for the host.
+// What a call of more than one launch takes the host, and each launch of it: a shorter call waits for the host.  (Calls that
+// are captured or part of a model do not; the estimate does not know them.)
 constexpr double kCall = 3.5, kLaunch = 3.2;
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
